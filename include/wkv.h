@@ -385,6 +385,150 @@ wkv_status wkv_decode_step_static(const wkv_decode_shape *shape, const void *q_n
                                   const void *v_new, void *k_cache, void *v_cache, int32_t *n_valid,
                                   float *out, void *hip_stream);
 
+/*
+ * ---- around the compression: rotary positions, the prompt's attention, eviction ---------------------------------
+ *
+ * Rotary positions.  Channels are turned in pairs by an angle a = position * inv_freq[i], i < rotary_dim / 2:
+ *     (x, y) -> amplitude * (x cos a - y sin a,  y cos a + x sin a)
+ * where pair i is channels (i, i + rotary_dim/2) or, with WKV_ROPE_INTERLEAVED, (2i, 2i+1); channels from rotary_dim on are
+ * copied.  The angle is reduced exactly (fixed point of 64 bits), so far positions lose nothing.
+ */
+/* wkv_rope_shape.flags.  WKV_ROPE_INVERSE turns by -a: it takes a rotation back (with an amplitude other than 1, up to its
+ * square), and is the gradient of the rotation. */
+#define WKV_ROPE_INTERLEAVED 1
+#define WKV_ROPE_INVERSE     2
+
+typedef struct {
+  int32_t batch;             /* >= 1                                                      */
+  int32_t n_tokens;          /* >= 0: rows per sequence; batch * n_tokens <= 2^25       */
+  int32_t n_q_heads;         /* >= 0; 0: no queries (q_in, q_out are not read)             */
+  int32_t n_kv_heads;        /* >= 0; 0: no keys                                          */
+  int32_t head_dim;          /* 64 or 128                                                 */
+  int32_t rotary_dim;        /* multiple of 16, 16 .. head_dim                            */
+  int32_t dtype;             /* wkv_dtype of all four tensors                             */
+  int32_t flags;             /* 0, or an OR of the WKV_ROPE_... flags above               */
+  double  amplitude;         /* factor of the rotated channels; 0 selects 1               */
+  const double *inv_freq;    /* host [rotary_dim / 2], finite; see wkv_rope_frequencies   */
+  int64_t q_stride_b, q_stride_h, q_stride_t;                /* q_in  [batch, n_q_heads, n_tokens, head_dim], elements */
+  int64_t q_out_stride_b, q_out_stride_h, q_out_stride_t;    /* q_out                      */
+  int64_t k_stride_b, k_stride_h, k_stride_t;                /* k_in  [batch, n_kv_heads, n_tokens, head_dim]          */
+  int64_t k_out_stride_b, k_out_stride_h, k_out_stride_t;    /* k_out, e.g. rows of a cache                            */
+} wkv_rope_shape;
+
+/*
+ *   positions     device int32 [batch, n_tokens], contiguous; a row whose position is negative (padding) is left as it is
+ *   q_in, k_in    device; e.g. the heads of one fused projection, by their strides
+ *   q_out, k_out  device; may be the inputs themselves, with the same strides (in place).  Otherwise no output may
+ *                 overlap an input or the other output.
+ * Computed in fp32, rounded once.
+ */
+wkv_status wkv_rope(const wkv_rope_shape *shape, const int32_t *positions, const void *q_in, void *q_out,
+                    const void *k_in, void *k_out, void *hip_stream);
+
+/*
+ * Inverse frequencies (host only): theta^(-2i / rotary_dim), changed for contexts `factor` times as long as the
+ * `original_len` tokens that a model was trained on.
+ *   WKV_ROPE_PLAIN       unchanged (factor and original_len are not read)
+ *   WKV_ROPE_LINEAR      all divided by factor
+ *   WKV_ROPE_BASE        theta replaced by theta * factor^(r / (r-2)): the slowest channel slows by factor, the fastest not
+ *   WKV_ROPE_PARTS       by channel number: channels that turn 32 times or more within original_len keep their frequency, those
+ *                        that turn once or less are divided by factor, with a linear ramp in between; amplitude
+ *                        0.1 ln(factor) + 1
+ *   WKV_ROPE_WAVELENGTH  by number of turns within original_len: 4 or more keep it, 1 or fewer are divided by factor, linear in
+ *                        the number of turns in between
+ *   inv_freq_out         host double [rotary_dim / 2]
+ *   amplitude_out        host double: 1 except for WKV_ROPE_PARTS
+ */
+typedef enum { WKV_ROPE_PLAIN = 0, WKV_ROPE_LINEAR = 1, WKV_ROPE_BASE = 2, WKV_ROPE_PARTS = 3, WKV_ROPE_WAVELENGTH = 4 } wkv_rope_scaling;
+wkv_status wkv_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling, double factor, int32_t original_len,
+                                double *inv_freq_out, double *amplitude_out);
+
+/*
+ * Attention over a prompt (Eq. 1 for every row, and its product with the values), the step that comes before the
+ * compression.  For sequence b, query row i < q_len[b] of head hq and the KV head h = hq / (n_q_heads / n_kv_heads):
+ *     out_i = sum_j softmax_j(scale * q_i . k_j) v_j,   j <= i + k_len[b] - q_len[b]
+ *     lse_i = ln sum_j exp(scale * q_i . k_j)
+ * The queries are the last q_len[b] tokens of the k_len[b] tokens in K and V: all of them (k_len = NULL), or a piece of a
+ * prompt that is taken in pieces, down to a single token.  A row that sees no key (k_len < q_len) gets out = 0, lse = -inf.
+ *
+ * Tensor layouts (strides in ELEMENTS; the head_dim axis always has stride 1):
+ *   q, out  [batch, n_q_heads,  rows, head_dim]   row i of sequence b lies at  b * stride_b + (q_start[b] + i) * stride_t
+ *   K, V    [batch, n_kv_heads, rows, head_dim]   likewise with k_start[b]; V has K's strides
+ * Padded batches and caches leave the starts NULL (0).  Packed sequences, one after the other in [rows, heads, head_dim],
+ * have stride_b = 0 and their first rows in q_start and k_start.  Rows of no sequence are neither read nor written.
+ */
+typedef struct {
+  int32_t batch;             /* 1 .. WKV_MAX_BATCH                                        */
+  int32_t n_q_heads;         /* Hq, multiple of n_kv_heads                                */
+  int32_t n_kv_heads;        /* Hkv                                                       */
+  int32_t head_dim;          /* d: 64 or 128                                              */
+  int32_t dtype;             /* wkv_dtype of q, K, V and out                              */
+  float   scale;             /* logit scale; 0 selects 1/sqrt(head_dim)                   */
+  int32_t lse_rows;          /* >= 0: normalisers of the last lse_rows rows of every sequence are written (0: none)        */
+  int32_t flags;             /* 0                                                         */
+  const int32_t *q_len;      /* host [batch], >= 0                                        */
+  const int32_t *k_len;      /* host [batch], >= 0, or NULL: q_len                        */
+  const int64_t *q_start;    /* host [batch], >= 0, or NULL: 0                            */
+  const int64_t *k_start;    /* host [batch], >= 0, or NULL: 0                            */
+  int64_t q_stride_b, q_stride_h, q_stride_t;
+  int64_t kv_stride_b, kv_stride_h, kv_stride_t;
+  int64_t out_stride_b, out_stride_h, out_stride_t;
+} wkv_attention_shape;
+
+/* Bytes of 256-byte-aligned device workspace wkv_prefill_attention needs; 0 for an invalid shape.  Its contents on entry are
+ * irrelevant and on return unspecified; calls that may overlap in time need workspaces of their own. */
+size_t wkv_attention_workspace_bytes(const wkv_attention_shape *shape);
+
+/*
+ *   q, k, v    device, layouts above.  Keys and values of the k_len rows must be finite; other rows may hold anything.
+ *   out        device, layout above; must not overlap the inputs
+ *   lse_out    device float32 [batch, n_q_heads, lse_rows] (contiguous), or NULL with lse_rows = 0: entry r belongs to row
+ *              q_len[b] - lse_rows + r, -inf where there is no such row.  With lse_rows = w_obs it is the lse_obs
+ *              that wkv_score and wkv_compress_groups take.
+ * Logits, softmax and output sums are fp32; 16-bit types round a probability (relative to the row's reference) to their own type for the
+ * product with the values, and the output once.  Results do not change from run to run.
+ */
+wkv_status wkv_prefill_attention(const wkv_attention_shape *shape, const void *q, const void *k, const void *v, void *out,
+                                 float *lse_out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * wkv_decode_step that also keeps, for every row of the cache, the attention weight it has received, summed over the steps and
+ * over the G query heads of its KV head: what wkv_cache_evict decides by.  With p_g(j) the softmax weights of
+ * this step, rows j < n = n_valid[b,h] and the new row n:
+ *     weights[b,h,j] += sum_g p_g(j)         weights[b,h,n] = sum_g p_g(n)         tok_idx[b,h,n] = position[b]
+ *   weights    device float32 [batch, n_kv_heads, capacity], contiguous; the caller's start values, e.g. 0, or the token
+ *              scores of Eq. 2 at the retained positions
+ *   tok_idx    device int32 [batch, n_kv_heads, capacity], contiguous, or NULL: token position of every cache row
+ *   position   device int32 [batch], or NULL with tok_idx: position of the new token
+ * Everything else as at wkv_decode_step, with a workspace of wkv_decode_weighted_workspace_bytes.  A (b, h) that cannot take the new row leaves its
+ * weights and positions as they are, too; where no row of a head weighs anything (all logits -inf), its weights count as 0.
+ */
+size_t wkv_decode_weighted_workspace_bytes(const wkv_decode_shape *shape);
+wkv_status wkv_decode_step_weighted(const wkv_decode_shape *shape, const void *q_new, const void *k_new, const void *v_new,
+                                    void *k_cache, void *v_cache, int32_t *n_valid, float *weights, int32_t *tok_idx,
+                                    const int32_t *position, float *out, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Eviction by accumulated attention weight: every (b, h) with n = n_valid[b,h] rows that exceed keep[b,h] is cut to keep[b,h]
+ * rows, the same ones in all layers of a group.  Rows whose position is among the last `recent` ones
+ * (tok_idx > max - recent, over the rows of the (b, h)) stay before others; then the larger weight stays, of equal weights the
+ * lower row (a weight of NaN is less than any other).  Kept rows below keep stay where they are; the r-th kept row from there on
+ * (ascending) moves into the r-th row below that is dropped, with its weight and position.  The rows of a cut cache are therefore in no order of
+ * position, which attention over them does not depend on; tok_idx tells it.
+ *   shape                the caches' shape; n_q_heads, scale and flags are not used
+ *   n_layers             1 .. WKV_MAX_LAYERS
+ *   k_caches, v_caches   host arrays [n_layers] of device pointers; in place
+ *   weights, tok_idx     device float32, int32 [batch, n_kv_heads, capacity], contiguous; in place
+ *   n_valid              device int32 [batch, n_kv_heads]; becomes keep[b,h] where rows were dropped
+ *   keep                 device int32 [batch, n_kv_heads]; negative: the (b, h) is left as it is
+ *   recent               >= 0
+ * A (b, h) whose n_valid is not in 0 .. capacity is left as it is.  Rows from the new count on hold what they held.
+ */
+size_t wkv_evict_workspace_bytes(const wkv_decode_shape *shape);
+wkv_status wkv_cache_evict(const wkv_decode_shape *shape, int32_t n_layers, void *const *k_caches, void *const *v_caches,
+                           float *weights, int32_t *tok_idx, int32_t *n_valid, const int32_t *keep, int32_t recent,
+                           void *workspace, size_t workspace_bytes, void *hip_stream);
+
 const char *wkv_status_string(wkv_status status);
 
 /* Message describing the most recent failure on the calling thread ("" if none). */

@@ -21,6 +21,8 @@ WKV_F32, WKV_BF16, WKV_F16 = 0, 1, 2
 WKV_KEEP_PADDING = 1          # Problem(flags=...): leave compact-cache rows past n_keep untouched
 WKV_SCORE_TWO_PASS, WKV_SCORE_SINGLE_READ, WKV_DEBUG_WAIT_GIVES_UP = 2, 4, 8      # Problem(flags=...)
 WKV_DECODE_KEEP_COUNT = 1     # DecodeShape(flags=...): n_valid is read but not advanced
+WKV_ROPE_INTERLEAVED, WKV_ROPE_INVERSE = 1, 2                                    # RopeShape(interleaved=..., inverse=...)
+WKV_ROPE_PLAIN, WKV_ROPE_LINEAR, WKV_ROPE_BASE, WKV_ROPE_PARTS, WKV_ROPE_WAVELENGTH = 0, 1, 2, 3, 4     # wkv_rope_frequencies
 WKV_MAX_BATCH, WKV_MAX_GROUPS, WKV_MAX_LAYERS, WKV_MAX_WIN = 64, 64, 64, 128
 WKV_MAX_OBS_ROWS, WKV_MAX_WINDOWS = 256, 32768
 WKV_N_STAGES = 4
@@ -29,7 +31,9 @@ STAGE_NAMES = ("score_stats", "score", "select", "gather")
 EXPORTS = ("wkv_get_dims", "wkv_workspace_bytes", "wkv_get_workspace_layout", "wkv_score", "wkv_window_pool",
            "wkv_topk_windows", "wkv_gather_group", "wkv_compress_group", "wkv_compress_groups",
            "wkv_compress_groups_profiled", "wkv_group_budgets", "wkv_status_string", "wkv_last_error",
-           "wkv_decode_workspace_bytes", "wkv_decode_step", "wkv_decode_step_static", "wkv_index_jaccard")
+           "wkv_decode_workspace_bytes", "wkv_decode_step", "wkv_decode_step_static", "wkv_index_jaccard",
+           "wkv_rope", "wkv_rope_frequencies", "wkv_attention_workspace_bytes", "wkv_prefill_attention",
+           "wkv_decode_weighted_workspace_bytes", "wkv_decode_step_weighted", "wkv_evict_workspace_bytes", "wkv_cache_evict")
 WKV_DECODE_STATIC_SCRATCH_BYTES = 8 << 20
 
 
@@ -60,6 +64,20 @@ class _DecodeShape(C.Structure):
                 ("flags", C.c_int32)]
 
 
+class _RopeShape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "n_tokens", "n_q_heads", "n_kv_heads", "head_dim", "rotary_dim", "dtype", "flags")] + \
+               [("amplitude", C.c_double), ("inv_freq", C.POINTER(C.c_double))] + \
+               [(f"{t}_stride_{x}", C.c_int64) for t in ("q", "q_out", "k", "k_out") for x in "bht"]
+
+
+class _AttentionShape(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("scale", C.c_float), ("lse_rows", C.c_int32), ("flags", C.c_int32),
+                ("q_len", C.POINTER(C.c_int32)), ("k_len", C.POINTER(C.c_int32)),
+                ("q_start", C.POINTER(C.c_int64)), ("k_start", C.POINTER(C.c_int64))] + \
+               [(f"{t}_stride_{x}", C.c_int64) for t in ("q", "kv", "out") for x in "bht"]
+
+
 class Dims(C.Structure):
     _fields_ = [("obs_rows", C.c_int32), ("t_stride", C.c_int32), ("nw_max", C.c_int32),
                 ("k_max", C.c_int32), ("nkeep_max", C.c_int32), ("total_tokens", C.c_int64)]
@@ -79,7 +97,8 @@ def native():
     if _calls is None:
         lib()
         module = importlib.import_module("._native", __name__)
-        module.bind(_current_stream, _structure, Problem, _Problem, DecodeShape, _DecodeShape)
+        module.bind(_current_stream, _structure, Problem, _Problem, DecodeShape, _DecodeShape, RopeShape, _RopeShape,
+                    AttentionShape, _AttentionShape)
         _calls = module
     return _calls
 
@@ -135,6 +154,16 @@ def lib() -> C.CDLL:
     l.wkv_decode_workspace_bytes.argtypes = [DP]; l.wkv_decode_workspace_bytes.restype = C.c_size_t
     l.wkv_decode_step.argtypes = [DP, VP, VP, VP, VP, VP, VP, VP, VP, C.c_size_t, VP]; l.wkv_decode_step.restype = C.c_int
     l.wkv_decode_step_static.argtypes = [DP, VP, VP, VP, VP, VP, VP, VP, VP]; l.wkv_decode_step_static.restype = C.c_int
+    RP, AP, VPP, SZ = C.POINTER(_RopeShape), C.POINTER(_AttentionShape), C.POINTER(VP), C.c_size_t
+    l.wkv_rope.argtypes = [RP, VP, VP, VP, VP, VP, VP]; l.wkv_rope.restype = C.c_int
+    l.wkv_rope_frequencies.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_int32, C.POINTER(C.c_double), C.POINTER(C.c_double)]
+    l.wkv_rope_frequencies.restype = C.c_int
+    l.wkv_attention_workspace_bytes.argtypes = [AP]; l.wkv_attention_workspace_bytes.restype = SZ
+    l.wkv_prefill_attention.argtypes = [AP, VP, VP, VP, VP, VP, VP, SZ, VP]; l.wkv_prefill_attention.restype = C.c_int
+    l.wkv_decode_weighted_workspace_bytes.argtypes = [DP]; l.wkv_decode_weighted_workspace_bytes.restype = SZ
+    l.wkv_decode_step_weighted.argtypes = [DP] + [VP] * 11 + [SZ, VP]; l.wkv_decode_step_weighted.restype = C.c_int
+    l.wkv_evict_workspace_bytes.argtypes = [DP]; l.wkv_evict_workspace_bytes.restype = SZ
+    l.wkv_cache_evict.argtypes = [DP, C.c_int32, VPP, VPP, VP, VP, VP, VP, C.c_int32, VP, SZ, VP]; l.wkv_cache_evict.restype = C.c_int
     l.wkv_status_string.argtypes = [C.c_int]; l.wkv_status_string.restype = C.c_char_p
     l.wkv_last_error.argtypes = []; l.wkv_last_error.restype = C.c_char_p
     _lib = l
@@ -319,3 +348,97 @@ def wkv_group_budgets(b_total: float, n_groups: int, lam: float) -> List[float]:
     _check(lib().wkv_group_budgets(b_total, n_groups, lam, out))
     return list(out)[:n_groups]
 
+
+
+class RopeShape:
+    """Mirrors ``wkv_rope_shape``.  Strides (b, h, t) in elements; ``None`` selects contiguous ``[B, H, T, d]`` tensors, for
+    the outputs the strides of the inputs.  ``inv_freq``: see :func:`wkv_rope_frequencies`."""
+
+    def __init__(self, *, batch: int, n_tokens: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int,
+                 inv_freq: Sequence[float], amplitude: float = 1.0, interleaved: bool = False, inverse: bool = False,
+                 q_strides=None, k_strides=None, q_out_strides=None, k_out_strides=None):
+        d = head_dim
+        rows = max(n_tokens, 1)
+        q_strides = q_strides or (n_q_heads * rows * d, rows * d, d)
+        k_strides = k_strides or (n_kv_heads * rows * d, rows * d, d)
+        self._keep = (C.c_double * max(len(inv_freq), 1))(*inv_freq)
+        flags = (WKV_ROPE_INTERLEAVED if interleaved else 0) | (WKV_ROPE_INVERSE if inverse else 0)
+        self.c = _RopeShape(batch, n_tokens, n_q_heads, n_kv_heads, d, 2 * len(inv_freq), dtype, flags, amplitude, self._keep,
+                            *q_strides, *(q_out_strides or q_strides), *k_strides, *(k_out_strides or k_strides))
+
+    def ref(self):
+        return C.byref(self.c)
+
+
+def wkv_rope_frequencies(rotary_dim: int, theta: float, scaling: int = WKV_ROPE_PLAIN, factor: float = 1.0, original_len: int = 0):
+    """(inverse frequencies, amplitude) for a :class:`RopeShape`."""
+    out, amplitude = (C.c_double * max(rotary_dim // 2, 1))(), C.c_double()
+    _check(lib().wkv_rope_frequencies(rotary_dim, theta, scaling, factor, original_len, out, C.byref(amplitude)))
+    return list(out), amplitude.value
+
+
+def wkv_rope(shape: RopeShape, positions, q_in, q_out, k_in, k_out, stream=None) -> None:
+    _check((_calls or native()).rope(shape, positions, q_in, q_out, k_in, k_out, stream))
+
+
+class AttentionShape:
+    """Mirrors ``wkv_attention_shape``.  Strides (b, h, t) in elements; ``None`` selects contiguous ``[B, H, L, d]`` tensors of the
+    longest sequence.  Packed sequences: strides with b = 0 and the first rows in ``q_start`` and ``k_start``."""
+
+    def __init__(self, *, q_len: Sequence[int], n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int,
+                 k_len: Optional[Sequence[int]] = None, q_start: Optional[Sequence[int]] = None, k_start: Optional[Sequence[int]] = None,
+                 scale: float = 0.0, lse_rows: int = 0, q_strides=None, kv_strides=None, out_strides=None, flags: int = 0):
+        B, d = len(q_len), head_dim
+        for name, xs in (("k_len", k_len), ("q_start", q_start), ("k_start", k_start)):
+            if xs is not None and len(xs) != B:
+                raise ValueError(f"{name} has {len(xs)} entries, q_len {B}")
+        rows, keys = max(q_len, default=0), max(k_len if k_len is not None else q_len, default=0)
+        q_strides = q_strides or (n_q_heads * max(rows, 1) * d, max(rows, 1) * d, d)
+        kv_strides = kv_strides or (n_kv_heads * max(keys, 1) * d, max(keys, 1) * d, d)
+
+        def i64(xs):
+            return (C.c_int64 * max(B, 1))(*[int(x) for x in xs]) if xs is not None else None
+
+        self._keep = [_i32(q_len), _i32(k_len) if k_len is not None else None, i64(q_start), i64(k_start)]
+        self.c = _AttentionShape(B, n_q_heads, n_kv_heads, d, dtype, scale, lse_rows, flags, *self._keep, *q_strides, *kv_strides,
+                                 *(out_strides or q_strides))
+
+    def ref(self):
+        return C.byref(self.c)
+
+
+def wkv_attention_workspace_bytes(shape: AttentionShape) -> int:
+    n = lib().wkv_attention_workspace_bytes(shape.ref())
+    if n == 0:
+        raise WkvError(WKV_ERR_INVALID_ARG, lib().wkv_last_error().decode())
+    return int(n)
+
+
+def wkv_prefill_attention(shape: AttentionShape, q, k, v, out, lse_out, workspace, stream=None) -> None:
+    """``lse_out``: float32 [batch, n_q_heads, lse_rows], or None with ``lse_rows=0``."""
+    _check((_calls or native()).prefill_attention(shape, q, k, v, out, lse_out, workspace, stream))
+
+
+def wkv_decode_weighted_workspace_bytes(shape: DecodeShape) -> int:
+    n = lib().wkv_decode_weighted_workspace_bytes(shape.ref())
+    if n == 0:
+        raise WkvError(WKV_ERR_INVALID_ARG, lib().wkv_last_error().decode())
+    return int(n)
+
+
+def wkv_decode_step_weighted(shape: DecodeShape, q_new, k_new, v_new, k_cache, v_cache, n_valid, weights, tok_idx, position, out,
+                             workspace, stream=None) -> None:
+    _check((_calls or native()).decode_step_weighted(shape, q_new, k_new, v_new, k_cache, v_cache, n_valid, weights, tok_idx, position,
+                                                     out, workspace, stream))
+
+
+def wkv_evict_workspace_bytes(shape: DecodeShape) -> int:
+    n = lib().wkv_evict_workspace_bytes(shape.ref())
+    if n == 0:
+        raise WkvError(WKV_ERR_INVALID_ARG, lib().wkv_last_error().decode())
+    return int(n)
+
+
+def wkv_cache_evict(shape: DecodeShape, k_caches, v_caches, weights, tok_idx, n_valid, keep, recent, workspace, stream=None) -> None:
+    """``k_caches``, ``v_caches``: the caches of the layers that share the row counts."""
+    _check((_calls or native()).cache_evict(shape, k_caches, v_caches, weights, tok_idx, n_valid, keep, recent, workspace, stream))

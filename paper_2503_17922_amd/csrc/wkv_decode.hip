@@ -19,18 +19,22 @@
 //   combine kernel  grid (B*Hkv, G): merges the key ranges of one query head and the new token (one dot
 //                   product; its row is appended to the caches here), normalises, writes fp32 output, bumps
 //                   the row count.
+#include <algorithm>
 #include <atomic>
 #include <mutex>
 #include <type_traits>
 
 #include "wkv_device.h"
+#include "wkv_operators.h"
 
 namespace wkv {
 
+#ifndef WKV_DECODE_WEIGHTED
 // Scratch memory of wkv_decode_step_static: part of the device image, one copy per GPU at that
 // GPU's own address.  In host code the name is only a handle for hipGetSymbolAddress; the device
 // address found there (per device, once) is what the kernels get.
 static __device__ __align__(256) unsigned char scratch[WKV_DECODE_STATIC_SCRATCH_BYTES];
+#endif
 
 constexpr int DEC_THREADS = 256;
 constexpr int DEC_WAVES = DEC_THREADS / 64;
@@ -126,6 +130,11 @@ __device__ __forceinline__ const float2 &part_stats(const DecodeShape &s, const 
   return *(const float2 *)((const char *)part + (s.stats_at + at * 8u));
 }
 
+// Where the logit of row j and head g is kept (WEIGHTS).
+__device__ __forceinline__ float *logit_at(const DecodeShape &s, const DecodeWeights &w, int bh, int g, int j) {
+  return w.logits + (((int64_t)bh * s.G + g) * ((int64_t)s.n_splits * s.chunk) + j);
+}
+
 // Merge the per-wave states in LDS ([wave][head][D outputs, m, l]) and store the workgroup's
 // partial result: one thread per (head, channel); the statistics are recomputed per thread.
 template <int D, int G>
@@ -175,12 +184,14 @@ struct KeyRange {
   }
 };
 
-template <typename T, int D, int G, bool STREAM>
+// WEIGHTS, here and below: the step that accumulates attention weights.  The logits and the row counts are kept for its merge launch, whose
+// workgroups add up the weights (a row's normaliser is not known before).  4 bytes a row and head, written and read, beside 2 * D elements.
+template <typename T, int D, int G, bool STREAM, bool WEIGHTS>
 __global__ __launch_bounds__(DEC_THREADS) void decode_partial_kernel(DecodeShape s, const T *__restrict__ q_new,
                                                                      const T *__restrict__ k_cache,
                                                                      const T *__restrict__ v_cache,
                                                                      const int32_t *__restrict__ n_valid,
-                                                                     float *__restrict__ part) {
+                                                                     float *__restrict__ part, DecodeWeights w) {
   constexpr int E = Piece<T>::E;
   constexpr int LPK = D / E;                 // lanes per row
   constexpr int KPT = 64 / LPK;              // rows per wave load instruction
@@ -191,6 +202,7 @@ __global__ __launch_bounds__(DEC_THREADS) void decode_partial_kernel(DecodeShape
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int slot = lane / LPK, piece = lane % LPK;
   const int n = item.n, c0 = split * s.chunk, cend = min(c0 + s.chunk, n < s.capacity ? n : 0);
+  if (WEIGHTS && split == 0 && threadIdx.x == 0) w.counts[bh] = n;
   if (nothing_to_do<G>(s, bh, split, n, c0, cend, part)) return;
 
   const T *kc = k_cache + (int64_t)b * s.sb + (int64_t)h * s.sh;
@@ -245,6 +257,7 @@ __global__ __launch_bounds__(DEC_THREADS) void decode_partial_kernel(DecodeShape
         for (int c = 0; c < E; ++c) a = fmaf(qv[g][c], kf[c], a);
         a = row_lanes_sum<LPK>(a);
         sc[u][g] = j < cend ? a : -INFINITY;
+        if (WEIGHTS && piece == g && j < cend) *logit_at(s, w, bh, g, j) = a;
       }
     }
 #pragma unroll
@@ -329,10 +342,10 @@ __device__ __forceinline__ void static_for(F &&f) {
   if constexpr (N > 0) { static_for<N - 1>(f); f(std::integral_constant<int, N - 1>{}); }
 }
 // STREAM: 0 plain loads, 1 values stream, 2 keys too (see launch_partial_g).
-template <int D, int G, bool F16, int STREAM, int NT>
+template <int D, int G, bool F16, int STREAM, int NT, bool WEIGHTS>
 __global__ __launch_bounds__(NT, 3) void decode_partial_mfma_kernel(
     DecodeShape s, const uint16_t *__restrict__ q_new, const uint16_t *k_cache,
-    const uint16_t *v_cache, const int32_t *__restrict__ n_valid, float *__restrict__ part) {
+    const uint16_t *v_cache, const int32_t *__restrict__ n_valid, float *__restrict__ part, DecodeWeights w) {
   constexpr int E = 8, WAVES = NT / 64;
   constexpr bool PAIRS = WAVES == DEC_WAVES;
   constexpr int LPK = D / E;                 // lanes per row (value side): 16 or 8
@@ -357,6 +370,7 @@ __global__ __launch_bounds__(NT, 3) void decode_partial_mfma_kernel(
     asm volatile("" ::"s"(kc), "s"(vc));
   }
   const int n = item.n, c0 = split * s.chunk, cend = min(c0 + s.chunk, n < s.capacity ? n : 0);
+  if (WEIGHTS && split == 0 && threadIdx.x == 0) w.counts[bh] = n;
   if (nothing_to_do<G>(s, bh, split, n, c0, cend, part)) return;
 
   // query rows as B fragments: lane (head col, quad) holds channels 32*ks + 8*quad .. +7; columns past the
@@ -411,6 +425,8 @@ __global__ __launch_bounds__(NT, 3) void decode_partial_mfma_kernel(
     float sc[4], pr[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) sc[e] = r0 + e < cend ? acc[e] * s.c1 : -INFINITY;
+    // (a whole piece of four rows also past the end: ranges are multiples of 64 rows)
+    if (WEIGHTS && col < G) *(float4 *)logit_at(s, w, bh, col, r0) = make_float4(sc[0], sc[1], sc[2], sc[3]);
     float mn = quads_max(fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3])));
     if (PAIRS) mn = fmaxf(m, mn);
     // -inf: every row so far has a logit of -inf (an infinite key, products that overflow) and weighs nothing
@@ -521,11 +537,65 @@ __global__ __launch_bounds__(NT, 3) void decode_partial_mfma_kernel(
 // own), 2.6 us with DPP reductions and six.
 // With few ranges one wave does it all and weighs them without LDS, a lane each (16 sequences of 500 rows 11.53 -> 11.28 us a layer; four
 // waves that each weigh up to 64 ranges for themselves, 9.55 -> 9.84 us for one sequence of 4128 rows: not so).
+// WEIGHTS: the workgroups from G on in y add up the attention weights of the cache's rows, each normalised for itself.
+constexpr int WEIGHT_ROWS = 4;        // rows of a thread at once
 template <typename T, int D, int NT>
+__device__ __forceinline__ void add_weights(const DecodeShape &s, const T *q_new, const T *k_new, const float *part, const DecodeWeights &w,
+                                            int bh, int b, int first_part, int n_parts) {
+  __shared__ float top[8], over_sum[8], logit_new[8];
+  const int n = w.counts[bh], tid = threadIdx.x, lane = tid & 63;
+  if (n < 0 || n >= s.capacity || (int64_t)first_part * (NT * WEIGHT_ROWS) > n) return;
+  for (int g = tid >> 6; g < s.G; g += NT / 64) {
+    float dot = 0.0f, m = -INFINITY, l = 0.0f;
+    for (int sp = lane; sp < s.n_splits; sp += 64) {
+      const float2 ml = part_stats(s, part, part_index(s, bh, sp, g));
+      merge_stats(m, l, ml.x, ml.y);
+    }
+#pragma unroll
+    for (int c = 0; c < D; c += 64)
+      dot = fmaf(Piece<T>::value(q_new + ((int64_t)bh * s.G + g) * D + c + lane), Piece<T>::value(k_new + (int64_t)bh * D + c + lane), dot);
+    const float logit = wave_sum(dot) * s.c1, mm = fmaxf(wave_max(m), logit);
+    const float sum = wave_sum(m == -INFINITY ? 0.0f : l * fast_exp2(m - mm)) + fast_exp2(logit - mm);
+    if (lane == 0) {
+      const bool none = mm == -INFINITY;              // no row weighs anything
+      top[g] = none ? 0.0f : mm;
+      over_sum[g] = none ? 0.0f : 1.0f / sum;
+      logit_new[g] = logit;
+    }
+  }
+  __syncthreads();
+  float *weights = w.weights + (int64_t)bh * s.capacity;
+  for (int64_t r0 = (int64_t)first_part * (NT * WEIGHT_ROWS); r0 <= n; r0 += (int64_t)n_parts * (NT * WEIGHT_ROWS)) {
+    float sum[WEIGHT_ROWS], old[WEIGHT_ROWS];
+#pragma unroll
+    for (int i = 0; i < WEIGHT_ROWS; ++i) {
+      sum[i] = 0.0f;
+      old[i] = weights[min(r0 + i * NT + tid, (int64_t)n)];
+    }
+    for (int g = 0; g < s.G; ++g) {
+      float x[WEIGHT_ROWS];
+#pragma unroll
+      for (int i = 0; i < WEIGHT_ROWS; ++i) {
+        const int64_t j = r0 + i * NT + tid;
+        x[i] = j < n ? *logit_at(s, w, bh, g, (int)j) : logit_new[g];
+      }
+#pragma unroll
+      for (int i = 0; i < WEIGHT_ROWS; ++i) sum[i] = fmaf(fast_exp2(x[i] - top[g]), over_sum[g], sum[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < WEIGHT_ROWS; ++i) {
+      const int64_t j = r0 + i * NT + tid;
+      if (j <= n) weights[j] = j < n ? old[i] + sum[i] : sum[i];
+      if (j == n && w.tok_idx) w.tok_idx[(int64_t)bh * s.capacity + n] = w.position[b];
+    }
+  }
+}
+
+template <typename T, int D, int NT, bool WEIGHTS>
 __global__ __launch_bounds__(NT) void decode_combine_kernel(DecodeShape s, const T *__restrict__ q_new,
                                                                      const T *__restrict__ k_new, const T *__restrict__ v_new,
                                                                      T *k_cache, T *v_cache, const float *__restrict__ part,
-                                                                     int32_t *n_valid, float *__restrict__ out) {
+                                                                     int32_t *n_valid, float *__restrict__ out, DecodeWeights dw) {
   constexpr int COLS = D / 4, GROUPS = NT / COLS, AHEAD = NT == 64 ? 4 : 6, WAVES = NT / 64;
   constexpr int E = Piece<T>::E, LPK = D / E;
   constexpr bool FEW = NT == 64;
@@ -537,6 +607,11 @@ __global__ __launch_bounds__(NT) void decode_combine_kernel(DecodeShape s, const
   asm volatile("" ::"s"(s.B), "s"(s.Hkv), "s"(s.G), "s"(s.d), "s"(s.kv_magic), "s"(s.capacity), "s"(s.n_splits), "s"(s.c1), "s"(s.sb), "s"(s.sh), "s"(s.st),
                "s"(s.keep_count), "s"(s.stats_at), "s"(q_new), "s"(k_new), "s"(v_new), "s"(k_cache), "s"(v_cache), "s"(part), "s"(n_valid), "s"(out));
   const int bh = blockIdx.x, g = blockIdx.y, b = divide(bh, s.kv_magic), h = bh - b * s.Hkv;
+  if constexpr (WEIGHTS)
+    if (g >= s.G) {
+      add_weights<T, D, NT>(s, q_new, k_new, part, dw, bh, b, g - s.G, gridDim.y - s.G);
+      return;
+    }
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int grp = tid / COLS, col = tid % COLS;
   const int64_t hq = (int64_t)bh * s.G + g;
@@ -654,9 +729,9 @@ __global__ __launch_bounds__(NT) void decode_combine_kernel(DecodeShape s, const
   if (g == 0 && tid == 0 && !s.keep_count && fits) n_valid[bh] = n + 1;
 }
 
-template <typename T, int D, int G>
+template <typename T, int D, int G, bool WEIGHTS>
 static void launch_partial_g(const DecodeShape &s, dim3 grid, const void *q, const void *kc, const void *vc,
-                             const int32_t *n_valid, float *part, hipStream_t stream) {
+                             const int32_t *n_valid, float *part, const DecodeWeights &w, hipStream_t stream) {
   // Where a model's caches exceed the memory-side cache, no row is found there at the next token, and the values, as both
   // caches in fp32, are best streamed.  How many layers there are and (n_valid is on the device) how many rows the library
   // cannot know: the line is that of 32 layers of full caches.  Us a layer with plain loads / with values streamed, where the rows
@@ -672,7 +747,7 @@ static void launch_partial_g(const DecodeShape &s, dim3 grid, const void *q, con
   const int64_t bytes = 2 * (int64_t)s.B * s.Hkv * s.capacity * D * (int64_t)sizeof(T);
   const int stream_level = bytes > MEMORY_CACHE_BYTES ? 2 : bytes > MEMORY_CACHE_BYTES / 32 ? 1 : 0;
 #define WKV_PARTIAL(KERNEL, E, NT) \
-  hipLaunchKernelGGL(KERNEL, grid, dim3(NT), 0, stream, s, (const E *)q, (const E *)kc, (const E *)vc, n_valid, part)
+  hipLaunchKernelGGL(KERNEL, grid, dim3(NT), 0, stream, s, (const E *)q, (const E *)kc, (const E *)vc, n_valid, part, w)
   if constexpr (sizeof(T) == 2) {   // bf16 / fp16: scores on the matrix pipe
     constexpr bool F16 = !__is_same(T, uint16_t);
     // Ranges of 128 rows by eight waves with a block each instead of four with two: half the arithmetic in a row, no state before the block, twice the
@@ -685,28 +760,28 @@ static void launch_partial_g(const DecodeShape &s, dim3 grid, const void *q, con
     constexpr bool WIDE = D == 128 && G <= 4;
     if constexpr (WIDE)
       if (s.chunk <= WIDE_THREADS / 64 * 16 && stream_level < 2) {
-        if (stream_level == 1) WKV_PARTIAL((decode_partial_mfma_kernel<D, G, F16, 1, WIDE_THREADS>), uint16_t, WIDE_THREADS);
-        else WKV_PARTIAL((decode_partial_mfma_kernel<D, G, F16, 0, WIDE_THREADS>), uint16_t, WIDE_THREADS);
+        if (stream_level == 1) WKV_PARTIAL((decode_partial_mfma_kernel<D, G, F16, 1, WIDE_THREADS, WEIGHTS>), uint16_t, WIDE_THREADS);
+        else WKV_PARTIAL((decode_partial_mfma_kernel<D, G, F16, 0, WIDE_THREADS, WEIGHTS>), uint16_t, WIDE_THREADS);
         return;
       }
     // (longer ranges than those are of caches that stream: as many as there can be of a cache, 128 rows each, are 16 MB)
     static_assert(!WIDE || (int64_t)DEC_MAX_SPLITS * 128 * 2 * D * (int64_t)sizeof(T) > MEMORY_CACHE_BYTES / 32, "plain loads");
-    if (stream_level == 2) WKV_PARTIAL((decode_partial_mfma_kernel<D, G, F16, 2, DEC_THREADS>), uint16_t, DEC_THREADS);
-    else if (WIDE || stream_level == 1) WKV_PARTIAL((decode_partial_mfma_kernel<D, G, F16, 1, DEC_THREADS>), uint16_t, DEC_THREADS);
-    else if constexpr (!WIDE) WKV_PARTIAL((decode_partial_mfma_kernel<D, G, F16, 0, DEC_THREADS>), uint16_t, DEC_THREADS);
+    if (stream_level == 2) WKV_PARTIAL((decode_partial_mfma_kernel<D, G, F16, 2, DEC_THREADS, WEIGHTS>), uint16_t, DEC_THREADS);
+    else if (WIDE || stream_level == 1) WKV_PARTIAL((decode_partial_mfma_kernel<D, G, F16, 1, DEC_THREADS, WEIGHTS>), uint16_t, DEC_THREADS);
+    else if constexpr (!WIDE) WKV_PARTIAL((decode_partial_mfma_kernel<D, G, F16, 0, DEC_THREADS, WEIGHTS>), uint16_t, DEC_THREADS);
   } else {
-    if (stream_level) WKV_PARTIAL((decode_partial_kernel<T, D, G, true>), T, DEC_THREADS);
-    else WKV_PARTIAL((decode_partial_kernel<T, D, G, false>), T, DEC_THREADS);
+    if (stream_level) WKV_PARTIAL((decode_partial_kernel<T, D, G, true, WEIGHTS>), T, DEC_THREADS);
+    else WKV_PARTIAL((decode_partial_kernel<T, D, G, false, WEIGHTS>), T, DEC_THREADS);
   }
 #undef WKV_PARTIAL
 }
 
-template <typename T, int D>
+template <typename T, int D, bool WEIGHTS>
 static hipError_t launch_decode_t(const DecodeShape &s, const void *q, const void *kn, const void *vn, void *kc, void *vc,
-                                  int32_t *n_valid, float *out, float *part, hipStream_t stream) {
+                                  int32_t *n_valid, float *out, float *part, const DecodeWeights &w, hipStream_t stream) {
   const dim3 grid(s.B * s.Hkv, s.n_splits);
 #define WKV_DEC_CASE(GG) \
-  case GG: launch_partial_g<T, D, GG>(s, grid, q, kc, vc, n_valid, part, stream); break;
+  case GG: launch_partial_g<T, D, GG, WEIGHTS>(s, grid, q, kc, vc, n_valid, part, w, stream); break;
   switch (s.G) {
     WKV_DEC_CASE(1) WKV_DEC_CASE(2) WKV_DEC_CASE(3) WKV_DEC_CASE(4) WKV_DEC_CASE(5) WKV_DEC_CASE(6)
     WKV_DEC_CASE(7) WKV_DEC_CASE(8)
@@ -717,25 +792,38 @@ static hipError_t launch_decode_t(const DecodeShape &s, const void *q, const voi
   if (e != hipSuccess) return e;
   // a wave reads eight ranges (16 at 64 channels) in its first round trip: with no more than that, one wave a head
   static_assert(DEC_MAX_SPLITS <= DEC_THREADS, "one thread per range");
-  const dim3 heads(s.B * s.Hkv, s.G);
+  // (by capacity, as the counts are on the device; a workgroup whose rows do not exist returns)
+  const auto weight_parts = [&](int nt) { return WEIGHTS ? (int)std::min<int64_t>(((int64_t)s.capacity + nt * WEIGHT_ROWS - 1) / (nt * WEIGHT_ROWS), 1024) : 0; };
 #define WKV_COMBINE(NT) \
-  hipLaunchKernelGGL((decode_combine_kernel<T, D, NT>), heads, dim3(NT), 0, stream, s, (const T *)q, (const T *)kn, (const T *)vn, \
-                     (T *)kc, (T *)vc, (const float *)part, n_valid, out)
+  hipLaunchKernelGGL((decode_combine_kernel<T, D, NT, WEIGHTS>), dim3(s.B * s.Hkv, s.G + weight_parts(NT)), dim3(NT), 0, stream, s, (const T *)q, \
+                     (const T *)kn, (const T *)vn, (T *)kc, (T *)vc, (const float *)part, n_valid, out, w)
   if (s.n_splits <= 1024 / D) WKV_COMBINE(64);
   else WKV_COMBINE(DEC_THREADS);
 #undef WKV_COMBINE
   return hipGetLastError();
 }
 
-hipError_t launch_decode(const DecodeShape &s, const void *q_new, const void *k_new, const void *v_new, void *k_cache,
-                         void *v_cache, int32_t *n_valid, float *out, float *part, hipStream_t stream) {
+template <bool WEIGHTS>
+static hipError_t launch_decode_as(const DecodeShape &s, const void *q_new, const void *k_new, const void *v_new, void *k_cache,
+                                   void *v_cache, int32_t *n_valid, float *out, float *part, const DecodeWeights &w, hipStream_t stream) {
 #define WKV_DEC_TYPE(TT) \
-  return s.d == 128 ? launch_decode_t<TT, 128>(s, q_new, k_new, v_new, k_cache, v_cache, n_valid, out, part, stream) \
-                    : launch_decode_t<TT, 64>(s, q_new, k_new, v_new, k_cache, v_cache, n_valid, out, part, stream);
+  return s.d == 128 ? launch_decode_t<TT, 128, WEIGHTS>(s, q_new, k_new, v_new, k_cache, v_cache, n_valid, out, part, w, stream) \
+                    : launch_decode_t<TT, 64, WEIGHTS>(s, q_new, k_new, v_new, k_cache, v_cache, n_valid, out, part, w, stream);
   if (s.dtype == WKV_BF16) WKV_DEC_TYPE(uint16_t)
   if (s.dtype == WKV_F16) WKV_DEC_TYPE(half_t)
   WKV_DEC_TYPE(float)
 #undef WKV_DEC_TYPE
+}
+
+#ifdef WKV_DECODE_WEIGHTED           // (compiled by wkv_decode_weighted.hip)
+hipError_t launch_decode_weighted(const DecodeShape &s, const void *q_new, const void *k_new, const void *v_new, void *k_cache,
+                                  void *v_cache, int32_t *n_valid, const DecodeWeights &w, float *out, float *part, hipStream_t stream) {
+  return launch_decode_as<true>(s, q_new, k_new, v_new, k_cache, v_cache, n_valid, out, part, w, stream);
+}
+#else
+hipError_t launch_decode(const DecodeShape &s, const void *q_new, const void *k_new, const void *v_new, void *k_cache,
+                         void *v_cache, int32_t *n_valid, float *out, float *part, hipStream_t stream) {
+  return launch_decode_as<false>(s, q_new, k_new, v_new, k_cache, v_cache, n_valid, out, part, DecodeWeights(), stream);
 }
 
 constexpr int MAX_DEVICES = 64;
@@ -763,5 +851,6 @@ hipError_t launch_decode_static(const DecodeShape &s, const void *q_new, const v
   // nothing in the array has to be cleared
   return launch_decode(s, q_new, k_new, v_new, k_cache, v_cache, n_valid, out, (float *)p, stream);
 }
+#endif
 
 }  // namespace wkv

@@ -1,0 +1,318 @@
+// Host side of the operators around the compression: argument validation, derived sizes, launch plans and the entry points.
+// Nothing in this file but the launchers' calls touches the GPU.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "wkv_operators.h"
+
+namespace wkv {
+
+namespace {
+
+inline bool misaligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+wkv_status invalid(const char *what) { set_error("%s", what); return WKV_ERR_INVALID_ARG; }
+wkv_status launched(hipError_t e, const char *what) {
+  if (e == hipSuccess) return WKV_OK;
+  set_error("%s launch: %s", what, hipGetErrorString(e));
+  return WKV_ERR_HIP;
+}
+bool known_dtype(int32_t dtype) {
+  if (dtype == WKV_F32 || dtype == WKV_BF16 || dtype == WKV_F16) return true;
+  set_error("unknown dtype %d", dtype);
+  return false;
+}
+// Row starts at multiples of 16 bytes, rows of head_dim channels that do not overlap.
+bool good_strides(int32_t dtype, int32_t head_dim, int64_t sb, int64_t sh, int64_t st, const char *what) {
+  const int64_t vec = 16 / elem_bytes(dtype);
+  if (sb < 0 || sh < 0 || st < 0 || sb % vec != 0 || sh % vec != 0 || st % vec != 0) {
+    set_error("%s strides must be non-negative multiples of %lld elements (16 bytes)", what, (long long)vec);
+    return false;
+  }
+  if (st < head_dim || sh < head_dim) { set_error("%s token and head strides must be >= head_dim", what); return false; }
+  return true;
+}
+wkv_status check_workspace(const void *ws, size_t bytes, size_t needed) {
+  if (!ws) { set_error("workspace is NULL"); return WKV_ERR_WORKSPACE; }
+  if (misaligned(ws, 256)) { set_error("workspace must be 256-byte aligned"); return WKV_ERR_WORKSPACE; }
+  if (bytes < needed) { set_error("workspace has %zu bytes, %zu needed", bytes, needed); return WKV_ERR_WORKSPACE; }
+  return WKV_OK;
+}
+size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
+
+// An angular frequency as turns per token modulo one, in units of 2^-64 turns.  (The division in 64 bits of mantissa: a position of
+// 2^31 leaves an error of 2^-33 turns of its frequency's 53 bits.)
+uint64_t turns_of(double inv_freq) {
+  const long double turns = (long double)inv_freq / 6.283185307179586476925286766559L;
+  const long double part = turns - floorl(turns);                // 0 <= part <= 1
+  const long double scaled = ldexpl(part, 64);
+  return scaled >= 18446744073709551615.0L ? 0 : (uint64_t)(scaled + 0.5L);
+}
+
+}  // namespace
+
+wkv_status plan_rope(const wkv_rope_shape *p, RopeArgs *a) {
+  set_error("");
+  if (!p) return invalid("shape is NULL");
+  if (p->batch < 1) { set_error("batch must be >= 1 (got %d)", p->batch); return WKV_ERR_INVALID_ARG; }
+  if (p->n_tokens < 0) return invalid("n_tokens must be >= 0");
+  if ((int64_t)p->batch * p->n_tokens > 1 << 25) { set_error("batch * n_tokens exceeds 2^25; split the call"); return WKV_ERR_UNSUPPORTED; }
+  if (p->n_q_heads < 0 || p->n_kv_heads < 0) return invalid("numbers of heads must be >= 0");
+  if (p->n_q_heads > 65535 || p->n_kv_heads > 65535) { set_error("more than 65535 heads"); return WKV_ERR_UNSUPPORTED; }
+  if (!known_dtype(p->dtype)) return WKV_ERR_INVALID_ARG;
+  if (p->head_dim != 64 && p->head_dim != 128) { set_error("head_dim %d is not supported (64 or 128)", p->head_dim); return WKV_ERR_UNSUPPORTED; }
+  if (p->rotary_dim < 1 || p->rotary_dim > p->head_dim) { set_error("rotary_dim %d outside [1, head_dim]", p->rotary_dim); return WKV_ERR_INVALID_ARG; }
+  if (p->rotary_dim % 16 != 0) { set_error("rotary_dim %d is not supported (a multiple of 16)", p->rotary_dim); return WKV_ERR_UNSUPPORTED; }
+  if (p->flags & ~(WKV_ROPE_INTERLEAVED | WKV_ROPE_INVERSE)) { set_error("unknown bits in flags (0x%x)", p->flags); return WKV_ERR_INVALID_ARG; }
+  if (!std::isfinite(p->amplitude) || std::fabs(p->amplitude) > 3.0e38) return invalid("amplitude must be finite (0 selects 1)");
+  if (!p->inv_freq) return invalid("inv_freq must be a non-NULL host array");
+  for (int32_t i = 0; i < p->rotary_dim / 2; ++i)
+    if (!std::isfinite(p->inv_freq[i])) { set_error("inv_freq[%d] is not finite", i); return WKV_ERR_INVALID_ARG; }
+  if (p->n_q_heads && (!good_strides(p->dtype, p->head_dim, p->q_stride_b, p->q_stride_h, p->q_stride_t, "q") ||
+                       !good_strides(p->dtype, p->head_dim, p->q_out_stride_b, p->q_out_stride_h, p->q_out_stride_t, "q_out")))
+    return WKV_ERR_INVALID_ARG;
+  if (p->n_kv_heads && (!good_strides(p->dtype, p->head_dim, p->k_stride_b, p->k_stride_h, p->k_stride_t, "k") ||
+                        !good_strides(p->dtype, p->head_dim, p->k_out_stride_b, p->k_out_stride_h, p->k_out_stride_t, "k_out")))
+    return WKV_ERR_INVALID_ARG;
+  std::memset(a, 0, sizeof(*a));
+  const int64_t e = elem_bytes(p->dtype);
+  a->q = {nullptr, nullptr, p->q_stride_b * e, p->q_stride_h * e, p->q_stride_t * e, p->q_out_stride_b * e, p->q_out_stride_h * e, p->q_out_stride_t * e};
+  a->k = {nullptr, nullptr, p->k_stride_b * e, p->k_stride_h * e, p->k_stride_t * e, p->k_out_stride_b * e, p->k_out_stride_h * e, p->k_out_stride_t * e};
+  for (int32_t i = 0; i < p->rotary_dim / 2; ++i) a->turns[i] = turns_of(p->inv_freq[i]);
+  a->batch = p->batch; a->n_tokens = p->n_tokens; a->q_heads = p->n_q_heads; a->kv_heads = p->n_kv_heads;
+  a->d = p->head_dim; a->rotary = p->rotary_dim; a->dtype = p->dtype;
+  a->interleaved = (p->flags & WKV_ROPE_INTERLEAVED) ? 1 : 0;
+  a->inverse = (p->flags & WKV_ROPE_INVERSE) ? 1 : 0;
+  a->amplitude = p->amplitude == 0.0 ? 1.0f : (float)p->amplitude;
+  return WKV_OK;
+}
+
+wkv_status plan_attention(const wkv_attention_shape *p, AttentionPlan *plan) {
+  set_error("");
+  if (!p) return invalid("shape is NULL");
+  if (!p->q_len) return invalid("q_len must be a non-NULL host array");
+  if (p->batch < 1) { set_error("batch must be >= 1 (got %d)", p->batch); return WKV_ERR_INVALID_ARG; }
+  if (p->batch > WKV_MAX_BATCH) { set_error("batch %d exceeds WKV_MAX_BATCH=%d; split the call", p->batch, WKV_MAX_BATCH); return WKV_ERR_UNSUPPORTED; }
+  if (p->n_kv_heads < 1 || p->n_q_heads < 1 || p->n_q_heads % p->n_kv_heads != 0) {
+    set_error("n_q_heads (%d) must be a positive multiple of n_kv_heads (%d)", p->n_q_heads, p->n_kv_heads); return WKV_ERR_INVALID_ARG;
+  }
+  if (!known_dtype(p->dtype)) return WKV_ERR_INVALID_ARG;
+  if (p->head_dim != 64 && p->head_dim != 128) { set_error("head_dim %d is not supported (64 or 128)", p->head_dim); return WKV_ERR_UNSUPPORTED; }
+  if (!(p->scale >= 0.0f) || std::isinf(p->scale)) return invalid("scale must be finite and >= 0 (0 selects 1/sqrt(head_dim))");
+  if (p->lse_rows < 0) return invalid("lse_rows must be >= 0");
+  if (p->flags != 0) { set_error("unknown bits in flags (0x%x)", p->flags); return WKV_ERR_INVALID_ARG; }
+  if (!good_strides(p->dtype, p->head_dim, p->q_stride_b, p->q_stride_h, p->q_stride_t, "q") ||
+      !good_strides(p->dtype, p->head_dim, p->kv_stride_b, p->kv_stride_h, p->kv_stride_t, "K and V") ||
+      !good_strides(p->dtype, p->head_dim, p->out_stride_b, p->out_stride_h, p->out_stride_t, "out"))
+    return WKV_ERR_INVALID_ARG;
+  // (the rows that a wave fetches of a tile are addressed by 32-bit offsets)
+  if (p->kv_stride_t * elem_bytes(p->dtype) * 64 > 0x7fffffff) { set_error("K and V token stride %lld is not supported", (long long)p->kv_stride_t); return WKV_ERR_UNSUPPORTED; }
+  AttentionArgs &a = plan->args;
+  std::memset(plan, 0, sizeof(*plan));
+  a.Hq = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = a.Hq / a.Hkv; a.d = p->head_dim; a.dtype = p->dtype; a.lse_rows = p->lse_rows;
+  a.n_seqs = p->batch;
+  const double scale = p->scale > 0.0f ? (double)p->scale : 1.0 / std::sqrt((double)p->head_dim);
+  a.c1 = (float)(scale * 1.4426950408889634074);
+  const int64_t e = elem_bytes(p->dtype);
+  a.q_sb = p->q_stride_b * e; a.q_sh = p->q_stride_h * e; a.q_st = p->q_stride_t * e;
+  a.kv_sb = p->kv_stride_b * e; a.kv_sh = p->kv_stride_h * e; a.kv_st = p->kv_stride_t * e;
+  a.o_sb = p->out_stride_b * e; a.o_sh = p->out_stride_h * e; a.o_st = p->out_stride_t * e;
+  for (int32_t b = 0; b < p->batch; ++b) {
+    AttentionSeq &s = a.seq[b];
+    s.b = b; s.q_len = p->q_len[b]; s.k_len = p->k_len ? p->k_len[b] : p->q_len[b];
+    s.q_start = p->q_start ? p->q_start[b] : 0; s.k_start = p->k_start ? p->k_start[b] : 0;
+    if (s.q_len < 0 || s.k_len < 0) { set_error("q_len[%d] = %d, k_len[%d] = %d: lengths must be >= 0", b, s.q_len, b, s.k_len); return WKV_ERR_INVALID_ARG; }
+    if (s.q_start < 0 || s.k_start < 0) { set_error("q_start[%d] and k_start[%d] must be >= 0", b, b); return WKV_ERR_INVALID_ARG; }
+    // (rows are divided by G through multiplication: row * G < 2^32)
+    if ((int64_t)s.q_len * a.G > ATT_MAX || s.k_len > ATT_MAX || ((int64_t)s.q_len * a.G + ATT_ROWS) * a.G > 0xffffffffll) {
+      set_error("sequence %d has too many rows or keys; split the call", b); return WKV_ERR_UNSUPPORTED;
+    }
+    // (a sequence without rows has a block for the normalisers of rows that do not exist)
+    s.blocks = (int32_t)std::max<int64_t>(ceil_div((int64_t)s.q_len * a.G, ATT_ROWS), p->lse_rows > 0 ? 1 : 0);
+  }
+  std::sort(a.seq, a.seq + p->batch, [](const AttentionSeq &x, const AttentionSeq &y) { return x.blocks != y.blocks ? x.blocks > y.blocks : x.b < y.b; });
+  int64_t items = 0;
+  for (int32_t i = 0; i < WKV_MAX_BATCH; ++i) {
+    if (i < p->batch) items += (int64_t)(a.seq[i].blocks - (i + 1 < p->batch ? a.seq[i + 1].blocks : 0)) * (i + 1) * a.Hkv;
+    if (items > 1 << 23) { set_error("more than 2^23 blocks of %d rows; split the call", ATT_ROWS); return WKV_ERR_UNSUPPORTED; }      // (launch grid limit)
+    a.ends[i] = (int32_t)items;
+  }
+  plan->items = (int32_t)items;
+  a.g_magic = division_magic(a.G);
+  plan->ws_bytes = 256;
+  return WKV_OK;
+}
+
+size_t decode_weighted_layout(const DecodeShape &s, size_t partial_bytes, size_t *counts_at, size_t *logits_at) {
+  const size_t rows = (size_t)s.B * s.Hkv;
+  *counts_at = round_up(partial_bytes);
+  *logits_at = round_up(*counts_at + rows * sizeof(int32_t));
+  return *logits_at + rows * s.G * s.n_splits * s.chunk * sizeof(float);
+}
+
+size_t evict_layout(int32_t rows, int32_t max_moves, size_t *moves_at) {
+  *moves_at = round_up((size_t)rows * sizeof(int32_t));
+  return *moves_at + (size_t)rows * max_moves * sizeof(int2);
+}
+// (row numbers and the ends of key ranges stay below 2^31)
+static wkv_status validate_cache(const wkv_decode_shape *shape, Decode *dc) {
+  const wkv_status st = validate_decode(shape, dc);
+  if (st != WKV_OK || dc->shape.capacity <= 1 << 30) return st;
+  set_error("capacity %d is not supported (at most 2^30 rows)", dc->shape.capacity);
+  return WKV_ERR_UNSUPPORTED;
+}
+
+// keep + (n - keep) rows of at most `capacity`: as many moves as the smaller part.
+static int32_t max_moves(int32_t capacity) { return std::max(capacity / 2, 1); }
+
+}  // namespace wkv
+
+using namespace wkv;
+
+extern "C" {
+
+wkv_status wkv_rope(const wkv_rope_shape *shape, const int32_t *positions, const void *q_in, void *q_out, const void *k_in, void *k_out,
+                    void *hip_stream) {
+  RopeArgs a;
+  const wkv_status st = plan_rope(shape, &a);
+  if (st != WKV_OK) return st;
+  if (a.n_tokens == 0 || (a.q_heads == 0 && a.kv_heads == 0)) return WKV_OK;
+  if (!positions) return invalid("positions is NULL");
+  if (misaligned(positions, 4)) return invalid("positions must be 4-byte aligned");
+  if (a.q_heads && (!q_in || !q_out)) return invalid("q_in / q_out is NULL");
+  if (a.kv_heads && (!k_in || !k_out)) return invalid("k_in / k_out is NULL");
+  if ((a.q_heads && (misaligned(q_in, 16) || misaligned(q_out, 16))) || (a.kv_heads && (misaligned(k_in, 16) || misaligned(k_out, 16))))
+    return invalid("the tensors must be 16-byte aligned");
+  a.q.in = q_in; a.q.out = q_out; a.k.in = k_in; a.k.out = k_out;
+  for (const RopeTensor *t : {a.q_heads ? &a.q : nullptr, a.kv_heads ? &a.k : nullptr})
+    if (t && t->in == t->out && (t->in_b != t->out_b || t->in_h != t->out_h || t->in_t != t->out_t))
+      return invalid("in place, input and output strides must be the same");
+  if (a.q_heads && a.kv_heads && q_out == k_out) return invalid("q_out and k_out are the same memory");
+  a.positions = positions;
+  return launched(launch_rope(a, (hipStream_t)hip_stream), "wkv_rope");
+}
+
+wkv_status wkv_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling, double factor, int32_t original_len, double *inv_freq_out,
+                                double *amplitude_out) {
+  set_error("");
+  if (!inv_freq_out || !amplitude_out) return invalid("inv_freq_out / amplitude_out is NULL");
+  if (rotary_dim < 2 || rotary_dim % 2 != 0 || rotary_dim > 65536) return invalid("rotary_dim must be even, 2 .. 65536");
+  if (!(theta > 1.0) || std::isinf(theta)) return invalid("theta must be finite and > 1");
+  if (scaling < WKV_ROPE_PLAIN || scaling > WKV_ROPE_WAVELENGTH) { set_error("unknown scaling %d", scaling); return WKV_ERR_INVALID_ARG; }
+  if (scaling != WKV_ROPE_PLAIN && (!(factor >= 1.0) || std::isinf(factor))) return invalid("factor must be finite and >= 1");
+  if ((scaling == WKV_ROPE_PARTS || scaling == WKV_ROPE_WAVELENGTH) && original_len < 1) return invalid("original_len must be >= 1");
+  if (scaling == WKV_ROPE_BASE && rotary_dim < 4) return invalid("WKV_ROPE_BASE needs a rotary_dim of at least 4");
+  const double r = rotary_dim, turn = 6.283185307179586477;
+  const double base = scaling == WKV_ROPE_BASE ? theta * std::pow(factor, r / (r - 2.0)) : theta;
+  // channel number (in pairs, real) that turns n times within the original context
+  auto channel_of = [&](double n) { return r * std::log(original_len / (n * turn)) / (2.0 * std::log(theta)); };
+  double lo = 0.0, hi = 0.0;
+  if (scaling == WKV_ROPE_PARTS) {
+    lo = std::max(std::floor(channel_of(32.0)), 0.0);
+    hi = std::min(std::ceil(channel_of(1.0)), r - 1.0);
+    if (hi <= lo) hi = lo + 0.001;
+  }
+  for (int32_t i = 0; i < rotary_dim / 2; ++i) {
+    const double f = std::pow(base, -2.0 * i / r);
+    double share = 1.0;                                  // of the unchanged frequency
+    if (scaling == WKV_ROPE_LINEAR) share = 0.0;
+    if (scaling == WKV_ROPE_PARTS) share = 1.0 - std::min(std::max((i - lo) / (hi - lo), 0.0), 1.0);
+    if (scaling == WKV_ROPE_WAVELENGTH) share = std::min(std::max((original_len * f / turn - 1.0) / (4.0 - 1.0), 0.0), 1.0);
+    inv_freq_out[i] = share == 1.0 ? f : f * share + f / factor * (1.0 - share);
+  }
+  *amplitude_out = scaling == WKV_ROPE_PARTS ? 0.1 * std::log(factor) + 1.0 : 1.0;
+  return WKV_OK;
+}
+
+size_t wkv_attention_workspace_bytes(const wkv_attention_shape *shape) {
+  AttentionPlan plan;
+  return plan_attention(shape, &plan) == WKV_OK ? plan.ws_bytes : 0;
+}
+
+wkv_status wkv_prefill_attention(const wkv_attention_shape *shape, const void *q, const void *k, const void *v, void *out, float *lse_out,
+                                 void *workspace, size_t workspace_bytes, void *hip_stream) {
+  AttentionPlan plan;
+  wkv_status st = plan_attention(shape, &plan);
+  if (st != WKV_OK) return st;
+  if (!q || !k || !v || !out) return invalid("q / k / v / out is NULL");
+  if (misaligned(q, 16) || misaligned(k, 16) || misaligned(v, 16) || misaligned(out, 16)) return invalid("q, k, v and out must be 16-byte aligned");
+  if (plan.args.lse_rows > 0 && !lse_out) return invalid("lse_out is NULL and lse_rows is not 0");
+  if (misaligned(lse_out, 4)) return invalid("lse_out must be 4-byte aligned");
+  if (out == q || out == k || out == v) return invalid("out must not overlap the inputs");
+  st = check_workspace(workspace, workspace_bytes, plan.ws_bytes);
+  if (st != WKV_OK) return st;
+  if (plan.items == 0) return WKV_OK;
+  return launched(launch_attention(plan, q, k, v, out, lse_out, workspace, (hipStream_t)hip_stream), "wkv_prefill_attention");
+}
+
+size_t wkv_decode_weighted_workspace_bytes(const wkv_decode_shape *shape) {
+  Decode dc;
+  size_t counts_at, logits_at;
+  if (validate_cache(shape, &dc) != WKV_OK) return 0;
+  return decode_weighted_layout(dc.shape, dc.ws_bytes, &counts_at, &logits_at);
+}
+
+wkv_status wkv_decode_step_weighted(const wkv_decode_shape *shape, const void *q_new, const void *k_new, const void *v_new, void *k_cache,
+                                    void *v_cache, int32_t *n_valid, float *weights, int32_t *tok_idx, const int32_t *position, float *out,
+                                    void *workspace, size_t workspace_bytes, void *hip_stream) {
+  Decode dc;
+  wkv_status st = validate_cache(shape, &dc);
+  if (st != WKV_OK) return st;
+  if (!q_new || !k_new || !v_new || !k_cache || !v_cache || !n_valid || !weights || !out)
+    return invalid("q_new / k_new / v_new / k_cache / v_cache / n_valid / weights / out is NULL");
+  if ((tok_idx == nullptr) != (position == nullptr)) return invalid("tok_idx and position go together: both or neither");
+  if (misaligned(q_new, 16) || misaligned(k_new, 16) || misaligned(v_new, 16) || misaligned(k_cache, 16) || misaligned(v_cache, 16))
+    return invalid("q_new, k_new, v_new and the caches must be 16-byte aligned");
+  if (misaligned(n_valid, 4) || misaligned(weights, 4) || misaligned(tok_idx, 4) || misaligned(position, 4) || misaligned(out, 4))
+    return invalid("n_valid, weights, tok_idx, position and out must be 4-byte aligned");
+  size_t counts_at, logits_at;
+  st = check_workspace(workspace, workspace_bytes, decode_weighted_layout(dc.shape, dc.ws_bytes, &counts_at, &logits_at));
+  if (st != WKV_OK) return st;
+  const DecodeWeights w = {weights, tok_idx, position, (int32_t *)((char *)workspace + counts_at), (float *)((char *)workspace + logits_at)};
+  return launched(launch_decode_weighted(dc.shape, q_new, k_new, v_new, k_cache, v_cache, n_valid, w, out, (float *)workspace, (hipStream_t)hip_stream),
+                  "wkv_decode_step_weighted");
+}
+
+size_t wkv_evict_workspace_bytes(const wkv_decode_shape *shape) {
+  Decode dc;
+  size_t moves_at;
+  if (validate_cache(shape, &dc) != WKV_OK) return 0;
+  return evict_layout(dc.shape.B * dc.shape.Hkv, max_moves(dc.shape.capacity), &moves_at);
+}
+
+wkv_status wkv_cache_evict(const wkv_decode_shape *shape, int32_t n_layers, void *const *k_caches, void *const *v_caches, float *weights,
+                           int32_t *tok_idx, int32_t *n_valid, const int32_t *keep, int32_t recent, void *workspace, size_t workspace_bytes,
+                           void *hip_stream) {
+  Decode dc;
+  wkv_status st = validate_cache(shape, &dc);
+  if (st != WKV_OK) return st;
+  if (n_layers < 1 || n_layers > WKV_MAX_LAYERS) { set_error("n_layers outside [1, %d]", WKV_MAX_LAYERS); return WKV_ERR_INVALID_ARG; }
+  if (!k_caches || !v_caches || !weights || !tok_idx || !n_valid || !keep) return invalid("k_caches / v_caches / weights / tok_idx / n_valid / keep is NULL");
+  if (recent < 0) return invalid("recent must be >= 0");
+  if (misaligned(weights, 4) || misaligned(tok_idx, 4) || misaligned(n_valid, 4) || misaligned(keep, 4))
+    return invalid("weights, tok_idx, n_valid and keep must be 4-byte aligned");
+  EvictLayers layers;
+  std::memset(&layers, 0, sizeof layers);
+  for (int32_t l = 0; l < n_layers; ++l) {
+    layers.k[l] = k_caches[l]; layers.v[l] = v_caches[l];
+    if (!layers.k[l] || !layers.v[l]) { set_error("cache of layer %d is NULL", l); return WKV_ERR_INVALID_ARG; }
+    if (misaligned(layers.k[l], 16) || misaligned(layers.v[l], 16)) { set_error("caches of layer %d must be 16-byte aligned", l); return WKV_ERR_INVALID_ARG; }
+  }
+  const DecodeShape &s = dc.shape;
+  EvictArgs a;
+  std::memset(&a, 0, sizeof a);
+  const int64_t e = elem_bytes(s.dtype);
+  a.rows = s.B * s.Hkv; a.Hkv = s.Hkv; a.capacity = s.capacity; a.recent = recent; a.row_bytes = (int32_t)(s.d * e);
+  a.hkv_magic = s.kv_magic;
+  a.sb = s.sb * e; a.sh = s.sh * e; a.st = s.st * e;
+  a.max_moves = max_moves(s.capacity);
+  size_t moves_at;
+  st = check_workspace(workspace, workspace_bytes, evict_layout(a.rows, a.max_moves, &moves_at));
+  if (st != WKV_OK) return st;
+  return launched(launch_evict(a, layers, n_layers, weights, tok_idx, n_valid, keep, (int32_t *)workspace, (int2 *)((char *)workspace + moves_at),
+                               (hipStream_t)hip_stream), "wkv_cache_evict");
+}
+
+}  // extern "C"

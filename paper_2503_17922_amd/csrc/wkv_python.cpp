@@ -13,7 +13,7 @@
 
 namespace {
 
-PyObject *s_c, *s_data_ptr, *s_numel, *s_element_size;        // interned attribute names
+PyObject *s_c, *s_data_ptr, *s_numel, *s_element_size, *s_get_device;        // interned attribute names
 PyObject *slow_stream;                                        // callable: the current stream by torch's public API
 PyObject *get_device, *get_raw_stream;                        // torch._C functions behind it, once torch has initialised the GPU
 PyObject *convert;                                            // callable (o, structure type): what ctypes takes from o.ref()
@@ -23,7 +23,7 @@ PyObject *convert;                                            // callable (o, st
 // may be copied or given another structure), of exactly this type; anything else goes to `convert`, which accepts and
 // refuses what a ctypes call of the same function does.
 struct Kind { PyObject *wrapper, *structure; };
-Kind problem_kind, shape_kind;
+Kind problem_kind, shape_kind, rope_kind, attention_kind;
 struct Structure {
   Py_buffer view;
   Structure() { view.obj = nullptr; }
@@ -43,6 +43,8 @@ struct Structure {
   }
   const wkv_problem *problem() const { return (const wkv_problem *)view.buf; }
   const wkv_decode_shape *shape() const { return (const wkv_decode_shape *)view.buf; }
+  const wkv_rope_shape *rope() const { return (const wkv_rope_shape *)view.buf; }
+  const wkv_attention_shape *attention() const { return (const wkv_attention_shape *)view.buf; }
 };
 
 bool pointer(PyObject *o, void **out) {
@@ -98,6 +100,16 @@ struct Pointers {
   }
 };
 
+// torch's functions for the current device and its stream, once torch has initialised the GPU.
+void find_torch_functions() {
+  PyObject *m = PyImport_ImportModule("torch._C");
+  PyObject *d = m ? PyObject_GetAttrString(m, "_cuda_getDevice") : nullptr;
+  PyObject *r = d ? PyObject_GetAttrString(m, "_cuda_getCurrentRawStream") : nullptr;
+  Py_XDECREF(m);
+  if (r) { get_device = d; get_raw_stream = r; }
+  else { Py_XDECREF(d); PyErr_Clear(); }       // a torch without them: the public API every time
+}
+
 bool stream_of(PyObject *o, void **out) {
   if (o != Py_None) {
     PyObject *i = PyNumber_Long(o);
@@ -120,16 +132,61 @@ bool stream_of(PyObject *o, void **out) {
   *out = PyLong_AsVoidPtr(v);
   Py_DECREF(v);
   if (PyErr_Occurred()) return false;
-  if (!get_raw_stream) {
-    PyObject *m = PyImport_ImportModule("torch._C");
-    PyObject *d = m ? PyObject_GetAttrString(m, "_cuda_getDevice") : nullptr;
-    PyObject *r = d ? PyObject_GetAttrString(m, "_cuda_getCurrentRawStream") : nullptr;
-    Py_XDECREF(m);
-    if (r) { get_device = d; get_raw_stream = r; }
-    else { Py_XDECREF(d); PyErr_Clear(); }       // a torch without them: the public API every time
-  }
+  if (!get_raw_stream) find_torch_functions();
   return true;
 }
+
+// The tensors of one call: all in the memory of one GPU, which is the current one (kernels are launched there).  Objects that are no
+// tensors (they have no get_device) are taken as they are.
+struct OneDevice {
+  long device = -1;
+  bool pointer(PyObject *o, void **out) {
+    if (o != Py_None) {
+      PyObject *v = PyObject_CallMethodNoArgs(o, s_get_device);
+      if (!v) {
+        if (!PyErr_ExceptionMatches(PyExc_AttributeError)) return false;
+        PyErr_Clear();
+      } else {
+        const long at = PyLong_AsLong(v);
+        Py_DECREF(v);
+        if (at == -1 && PyErr_Occurred()) return false;
+        if (at < 0) { PyErr_SetString(PyExc_ValueError, "expected tensors in GPU memory"); return false; }
+        if (device >= 0 && at != device) { PyErr_Format(PyExc_ValueError, "tensors of one call on devices %ld and %ld", device, at); return false; }
+        device = at;
+      }
+    }
+    return ::pointer(o, out);
+  }
+  template <int CAP>
+  bool pointers(PyObject *seq, Pointers<CAP> &p) {
+    std::memset(p.p, 0, sizeof p.p);
+    PyObject *f = PySequence_Fast(seq, "expected a sequence of tensors");
+    if (!f) return false;
+    p.n = PySequence_Fast_GET_SIZE(f);
+    bool ok = true;
+    for (Py_ssize_t i = 0; ok && i < p.n && i < CAP; ++i) ok = pointer(PySequence_Fast_GET_ITEM(f, i), &p.p[i]);
+    Py_DECREF(f);
+    return ok;
+  }
+  bool workspace(PyObject *o, void **out, size_t *bytes) {
+    void *same;
+    return pointer(o, &same) && ::workspace(o, out, bytes);
+  }
+  // The stream, and whether the tensors are where it is.
+  bool stream(PyObject *o, void **out) {
+    if (!stream_of(o, out)) return false;
+    if (device < 0) return true;
+    if (!get_device) find_torch_functions();
+    if (!get_device) return true;
+    PyObject *d = PyObject_CallNoArgs(get_device);
+    if (!d) return false;
+    const long current = PyLong_AsLong(d);
+    Py_DECREF(d);
+    if (current == -1 && PyErr_Occurred()) return false;
+    if (current != device) { PyErr_Format(PyExc_ValueError, "tensors on device %ld, the current device is %ld", device, current); return false; }
+    return true;
+  }
+};
 
 bool arity(Py_ssize_t n, Py_ssize_t want) {
   if (n == want) return true;
@@ -265,11 +322,68 @@ PyObject *compress_groups(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
-// (slow_stream, convert, Problem, its structure, DecodeShape, its structure)
+// (shape, positions, q_in, q_out, k_in, k_out, stream)
+PyObject *rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  Structure sh;
+  OneDevice at;
+  void *t[5], *st;
+  if (!arity(n, 7) || !sh.fill(a[0], rope_kind)) return nullptr;
+  for (int i = 0; i < 5; ++i) if (!at.pointer(a[1 + i], &t[i])) return nullptr;
+  if (!at.stream(a[6], &st)) return nullptr;
+  return call([&] { return wkv_rope(sh.rope(), (const int32_t *)t[0], t[1], t[2], t[3], t[4], st); });
+}
+
+// (shape, q, k, v, out, lse_out, workspace, stream)
+PyObject *prefill_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  Structure sh;
+  OneDevice at;
+  void *t[5], *ws, *st;
+  size_t bytes;
+  if (!arity(n, 8) || !sh.fill(a[0], attention_kind)) return nullptr;
+  for (int i = 0; i < 5; ++i) if (!at.pointer(a[1 + i], &t[i])) return nullptr;
+  if (!at.workspace(a[6], &ws, &bytes) || !at.stream(a[7], &st)) return nullptr;
+  return call([&] { return wkv_prefill_attention(sh.attention(), t[0], t[1], t[2], t[3], (float *)t[4], ws, bytes, st); });
+}
+
+// (shape, q_new, k_new, v_new, k_cache, v_cache, n_valid, weights, tok_idx, position, out, workspace, stream)
+PyObject *decode_step_weighted(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  Structure sh;
+  OneDevice at;
+  void *t[10], *ws, *st;
+  size_t bytes;
+  if (!arity(n, 13) || !sh.fill(a[0], shape_kind)) return nullptr;
+  for (int i = 0; i < 10; ++i) if (!at.pointer(a[1 + i], &t[i])) return nullptr;
+  if (!at.workspace(a[11], &ws, &bytes) || !at.stream(a[12], &st)) return nullptr;
+  return call([&] {
+    return wkv_decode_step_weighted(sh.shape(), t[0], t[1], t[2], t[3], t[4], (int32_t *)t[5], (float *)t[6], (int32_t *)t[7],
+                                    (const int32_t *)t[8], (float *)t[9], ws, bytes, st);
+  });
+}
+
+// (shape, k_caches, v_caches, weights, tok_idx, n_valid, keep, recent, workspace, stream)
+PyObject *cache_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  Structure sh;
+  OneDevice at;
+  void *t[4], *ws, *st;
+  size_t bytes;
+  int32_t recent;
+  Pointers<WKV_MAX_LAYERS> k, v;
+  if (!arity(n, 10) || !sh.fill(a[0], shape_kind) || !at.pointers(a[1], k) || !at.pointers(a[2], v)) return nullptr;
+  for (int i = 0; i < 4; ++i) if (!at.pointer(a[3 + i], &t[i])) return nullptr;
+  if (!integer(a[7], &recent) || !at.workspace(a[8], &ws, &bytes) || !at.stream(a[9], &st)) return nullptr;
+  if (k.n != v.n) { PyErr_SetString(PyExc_ValueError, "as many key caches as value caches"); return nullptr; }
+  const int32_t layers = (int32_t)(k.n > WKV_MAX_LAYERS ? WKV_MAX_LAYERS + 1 : k.n);
+  return call([&] {
+    return wkv_cache_evict(sh.shape(), layers, k.p, v.p, (float *)t[0], (int32_t *)t[1], (int32_t *)t[2], (const int32_t *)t[3], recent, ws, bytes, st);
+  });
+}
+
+// (slow_stream, convert, then each class of structures and the ctypes structure it wraps: Problem, DecodeShape, RopeShape, AttentionShape)
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  if (!arity(n, 6)) return nullptr;
-  PyObject **to[6] = {&slow_stream, &convert, &problem_kind.wrapper, &problem_kind.structure, &shape_kind.wrapper, &shape_kind.structure};
-  for (int i = 0; i < 6; ++i) {
+  if (!arity(n, 10)) return nullptr;
+  PyObject **to[10] = {&slow_stream, &convert, &problem_kind.wrapper, &problem_kind.structure, &shape_kind.wrapper, &shape_kind.structure,
+                       &rope_kind.wrapper, &rope_kind.structure, &attention_kind.wrapper, &attention_kind.structure};
+  for (int i = 0; i < 10; ++i) {
     Py_INCREF(a[i]);
     Py_XSETREF(*to[i], a[i]);
   }
@@ -279,6 +393,7 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(decode_step), FAST(decode_step_static), FAST(score), FAST(window_pool), FAST(topk_windows),
                          FAST(gather_group), FAST(compress_group), FAST(compress_groups),
+                         FAST(rope), FAST(prefill_attention), FAST(decode_step_weighted), FAST(cache_evict),
                          FAST(bind), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -289,6 +404,7 @@ PyMODINIT_FUNC PyInit__native(void) {
   s_data_ptr = PyUnicode_InternFromString("data_ptr");
   s_numel = PyUnicode_InternFromString("numel");
   s_element_size = PyUnicode_InternFromString("element_size");
-  if (!s_c || !s_data_ptr || !s_numel || !s_element_size) return nullptr;
+  s_get_device = PyUnicode_InternFromString("get_device");
+  if (!s_c || !s_data_ptr || !s_numel || !s_element_size || !s_get_device) return nullptr;
   return PyModule_Create(&module);
 }

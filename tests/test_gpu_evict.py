@@ -1,0 +1,154 @@
+"""wkv_cache_evict against its definition: protected rows, then the larger weight, then the lower row; the moves; everything else left alone."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2503_17922_amd as W
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {W.WKV_F32: torch.float32, W.WKV_BF16: torch.bfloat16, W.WKV_F16: torch.float16}
+
+
+def expected(weights, tok, n, keep, recent):
+    """Source row of every row of the cut cache, for one (sequence, KV head) on the host; None: left as it is."""
+    if keep < 0 or n < 0 or n > len(weights) or n <= keep:
+        return None
+    w, t = weights[:n].astype(np.float64), tok[:n].astype(np.int64)
+    protected = t > t.max() - recent
+    w = np.where(np.isnan(w), -math.inf, w)
+    is_nan = np.isnan(weights[:n])
+    order = np.lexsort((np.arange(n), -w, is_nan, ~protected))     # last key first
+    kept = np.sort(order[:keep])
+    late, holes = kept[kept >= keep], np.setdiff1d(np.arange(keep), kept)
+    source = np.arange(keep)
+    source[holes] = late
+    return source
+
+
+class State:
+    def __init__(self, device, counts, keep, recent, H=2, d=128, dtype=W.WKV_BF16, cap=None, layers=2, layout="bhtd", seed=1, weights=None, tok=None):
+        g = torch.Generator(device=device).manual_seed(seed)
+        t, B = TYPES[dtype], len(counts)
+        self.n = torch.tensor(counts, dtype=torch.int32, device=device)
+        if self.n.dim() == 1:
+            self.n = self.n[:, None].repeat(1, H)
+        cap = cap or int(self.n.max()) + 3
+        shape = (B, H, cap, d) if layout == "bhtd" else (B, cap, H, d)
+        mk = lambda: torch.randn(shape, device=device, generator=g).to(t)
+        fix = (lambda x: x) if layout == "bhtd" else (lambda x: x.transpose(1, 2))
+        self.k, self.v = [fix(mk()) for _ in range(layers)], [fix(mk()) for _ in range(layers)]
+        strides = None if layout == "bhtd" else (cap * H * d, d, H * d)
+        self.w = weights if weights is not None else torch.rand((B, H, cap), device=device, generator=g) ** 4
+        self.tok = tok if tok is not None else torch.cumsum(torch.randint(1, 5, (B, H, cap), device=device, generator=g), -1).to(torch.int32)
+        self.keep = torch.as_tensor(keep, dtype=torch.int32, device=device).expand(B, H).contiguous()
+        self.recent = recent
+        self.shape = W.DecodeShape(batch=B, n_q_heads=H, n_kv_heads=H, head_dim=d, dtype=dtype, capacity=cap, cache_strides=strides)
+        self.ws = torch.full((W.wkv_evict_workspace_bytes(self.shape),), 0xff, dtype=torch.uint8, device=device)
+
+    def call(self):
+        W.wkv_cache_evict(self.shape, self.k, self.v, self.w, self.tok, self.n, self.keep, self.recent, self.ws)
+
+    def tensors(self):
+        return self.k + self.v + [self.w, self.tok]
+
+    def check(self, call=None):
+        before = [x.clone() for x in self.tensors()]
+        n, keep = self.n.cpu().numpy(), self.keep.cpu().numpy()
+        w, tok = self.w.cpu().numpy(), self.tok.cpu().numpy()
+        (call or self.call)()
+        torch.cuda.synchronize()
+        want_n = n.copy()
+        for b in range(n.shape[0]):
+            for h in range(n.shape[1]):
+                source = expected(w[b, h], tok[b, h], int(n[b, h]), int(keep[b, h]), self.recent)
+                if source is None:
+                    continue
+                want_n[b, h] = keep[b, h]
+                ii = torch.from_numpy(source).to(self.n.device)
+                for x in before:
+                    x[b, h, :len(source)] = x[b, h][ii]
+        assert np.array_equal(self.n.cpu().numpy(), want_n)
+        for i, (x, y) in enumerate(zip(self.tensors(), before)):
+            as_bits = (lambda z: z.view(torch.int32)) if x.dtype == torch.float32 else (lambda z: z)
+            assert torch.equal(as_bits(x), as_bits(y)), f"tensor {i}"
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("layout", ["bhtd", "bthd"])
+def test_types_and_layouts(device, dtype, d, layout):
+    State(device, [100, 70, 64], 64, 8, d=d, dtype=dtype, layout=layout).check()
+
+
+@pytest.mark.parametrize("counts,keep", [([1], 0), ([2], 1), ([64], 63), ([65], 64), ([1000], 1), ([1000], 500), ([1025, 1024, 1023], 1000),
+                                         ([4097, 4096], 4096), ([9000], 8191), ([40000], 30000), ([70001], 123)])
+@pytest.mark.parametrize("recent", [0, 1, 32])
+def test_sizes(device, counts, keep, recent):
+    State(device, counts, keep, recent, d=64, layers=1).check()
+
+
+def test_a_row_at_a_time(device):
+    s = State(device, [120, 90], 119, 16)
+    for _ in range(5):
+        s.check()
+        s.keep -= 1
+
+
+def test_counts_and_budgets_of_their_own(device):
+    State(device, [[50, 0], [-1, 53], [60, 20], [54, 7]], [[40, 0], [3, 3], [-1, 20], [0, 100]], 4, cap=53).check()
+
+
+@pytest.mark.parametrize("levels", [1, 2, 5])
+def test_equal_weights_go_by_the_lower_row(device, levels):
+    g = torch.Generator(device=device).manual_seed(7)
+    w = torch.randint(0, levels, (2, 2, 3000), device=device, generator=g).float()
+    State(device, [3000, 1500], 1111, 20, cap=3000, weights=w, seed=2).check()
+
+
+def test_every_kind_of_weight(device):
+    g = torch.Generator(device=device).manual_seed(8)
+    special = torch.tensor([math.nan, -math.nan, math.inf, -math.inf, 0.0, -0.0, 1e-45, -1e-45, 3.4e38, -3.4e38, 1.0, -1.0], device=device)
+    w = special[torch.randint(0, 12, (1, 2, 600), device=device, generator=g)]
+    for keep in (0, 40, 90, 150, 333, 550):
+        State(device, [600], keep, 10, cap=600, weights=w.clone(), seed=3).check()
+
+
+def test_more_protected_rows_than_fit(device):
+    State(device, [500], 100, 2 ** 31 - 1).check()                       # all protected: the lower rows stay
+    State(device, [500], 100, 300).check()
+
+
+@pytest.mark.parametrize("first", [-2 ** 31, 2 ** 31 - 400])
+def test_positions_at_the_ends_of_their_type(device, first):
+    tok = (torch.arange(400, device=device, dtype=torch.int64) + first).to(torch.int32).repeat(1, 2, 1)
+    State(device, [400], 200, 50, cap=400, tok=tok).check()
+
+
+def test_rows_in_no_order_and_equal_positions(device):
+    g = torch.Generator(device=device).manual_seed(4)
+    State(device, [777], 300, 40, cap=777, tok=torch.randint(0, 300, (1, 2, 777), device=device, generator=g, dtype=torch.int32)).check()
+
+
+def test_many_layers_and_the_same_cache_twice(device):
+    s = State(device, [300, 280], 256, 16, layers=64, d=64)
+    s.check()
+    s = State(device, [300], 200, 16, layers=2)
+    s.k[1], s.v[1] = s.k[0], s.v[0]
+    s.check()
+
+
+def test_captured_and_replayed(device):
+    s = State(device, [300, 250], 240, 16)
+    s.call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s.call()
+    for step in range(3):
+        s.n += 30 + step
+        s.w.copy_(torch.rand_like(s.w))
+        s.tok.copy_(torch.randint(0, 10 ** 6, s.tok.shape, device=device))
+        s.check(graph.replay)
