@@ -59,46 +59,65 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b) {
   }
 }
 
+// Which block of which (sequence, KV head) work item `item` is, and what follows for the keys.
+struct Block {
+  AttentionSeq sq;
+  int h, block, past, n_rows, n_tiles, n_splits;
+  const AttentionArgs &a;
+  __device__ __forceinline__ Block(const AttentionArgs &args, int item, int tile_keys) : a(args) {
+    const int lane = threadIdx.x & 63;
+    const int end = lane < a.n_seqs ? a.ends[lane] : 0x7fffffff;
+    const int seg = __builtin_amdgcn_readfirstlane(__builtin_popcountll(__ballot(item >= end)));
+    const int rel = item - (seg ? a.ends[seg - 1] : 0);
+    const int level_items = (seg + 1) * a.Hkv;
+    const int level = (int)((uint32_t)rel / (uint32_t)level_items), at = rel - level * level_items;
+    const int si = (int)((uint32_t)at / (uint32_t)a.Hkv);
+    h = at - si * a.Hkv;
+    sq = a.seq[si];
+    block = a.seq[seg].blocks - 1 - level;
+    past = sq.k_len - sq.q_len;
+    n_rows = sq.q_len * a.G;
+    n_tiles = n_rows ? (sees(min((block + 1) * ATT_ROWS, n_rows) - 1) + tile_keys - 1) / tile_keys : 0;
+    n_splits = a.splits == 1 ? 1 : max((n_tiles + a.chunk - 1) / a.chunk, 1);
+  }
+  __device__ __forceinline__ int query(int r) const { return divide((uint32_t)r, a.g_magic); }
+  __device__ __forceinline__ int sees(int r) const { return min(max(query(r) + past + 1, 0), sq.k_len); }      // keys that row r sees
+};
+
+// Natural logarithm of a row's sum, from its base-2 reference; no key weighs anything: -inf.
+__device__ __forceinline__ float row_lse(float m, float l) { return l == 0.0f ? -INFINITY : (m + fast_log2(l)) * 0.69314718055994531f; }
+
 constexpr float ATT_GROW = 8.0f;      // a row's reference moves when a logit exceeds it by this (base 2): probabilities up to 2^8
 
 template <int D, int DT>
 __global__ __launch_bounds__(256, 2) void prefill_kernel(AttentionArgs a, const char *__restrict__ q, const char *__restrict__ k,
-                                                         const char *__restrict__ v, char *__restrict__ out, float *__restrict__ lse) {
+                                                         const char *__restrict__ v, char *__restrict__ out, float *__restrict__ lse,
+                                                         float *__restrict__ part, float2 *__restrict__ stats) {
   using C = Att<D, DT>;
   constexpr int KS = C::KS, KT = C::KT, VT = C::VT;
   __shared__ __attribute__((aligned(1024))) char ring[C::STAGES * C::STAGE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
 
-  // ---- which block of which KV head
-  const int item = blockIdx.x;
-  const int end = lane < a.n_seqs ? a.ends[lane] : 0x7fffffff;
-  const int seg = __builtin_amdgcn_readfirstlane(__builtin_popcountll(__ballot(item >= end)));
-  const int rel = item - (seg ? a.ends[seg - 1] : 0);
-  const int level_items = (seg + 1) * a.Hkv;
-  const int level = (int)((uint32_t)rel / (uint32_t)level_items), at = rel - level * level_items;
-  const int si = (int)((uint32_t)at / (uint32_t)a.Hkv), h = at - si * a.Hkv;
-  const AttentionSeq &sq = a.seq[si];
-  const int block = a.seq[seg].blocks - 1 - level;
-  const int q_len = sq.q_len, k_len = sq.k_len, past = k_len - q_len;
-  const int n_rows = q_len * a.G;
-
-  if (block == 0)                        // normalisers of rows that do not exist
+  // ---- which block of which KV head, and which of its key tiles
+  const Block it(a, blockIdx.x, C::KEYS);
+  const AttentionSeq &sq = it.sq;
+  const int h = it.h, block = it.block, q_len = sq.q_len, k_len = sq.k_len, n_rows = it.n_rows, split = blockIdx.y;
+  if (split >= it.n_splits) return;
+  if (block == 0 && split == 0)          // normalisers of rows that do not exist
     for (int i = threadIdx.x; i < (a.lse_rows - q_len) * a.G; i += C::NT) {
       const int r = i / a.G, g = i - r * a.G;
       lse[((int64_t)sq.b * a.Hq + h * a.G + g) * a.lse_rows + r] = -INFINITY;
     }
   if (n_rows == 0) return;
+  const int t_begin = split ? split * a.chunk : 0, t_end = it.n_splits == 1 ? it.n_tiles : min(t_begin + a.chunk, it.n_tiles);
 
   // ---- this lane's row
-  const int first_row = block * ATT_ROWS, last_row = min(first_row + ATT_ROWS, n_rows) - 1;
-  const int wave_first = min(first_row + wave * 32, n_rows - 1), wave_last = min(first_row + wave * 32 + 31, n_rows - 1);
+  const int first_row = block * ATT_ROWS;
   const int row = min(first_row + wave * 32 + col, n_rows - 1);
-  const int qi = divide((uint32_t)row, a.g_magic), g = row - qi * a.G;
-  auto sees = [&](int r) { return min(max(divide((uint32_t)r, a.g_magic) + past + 1, 0), k_len); };      // keys that row r sees
-  const int seen = sees(row), wave_least = sees(wave_first), wave_most = first_row + wave * 32 < n_rows ? sees(wave_last) : 0;
-  const int n_keys = sees(last_row);
-  const int n_tiles = (n_keys + C::KEYS - 1) / C::KEYS;
+  const int qi = it.query(row), g = row - qi * a.G;
+  const int seen = it.sees(row), wave_least = it.sees(min(first_row + wave * 32, n_rows - 1));
+  const int wave_most = first_row + wave * 32 < n_rows ? it.sees(min(first_row + wave * 32 + 31, n_rows - 1)) : 0;
 
   // ---- the key and value stream
   const char *kb = k + (sq.b * a.kv_sb + h * a.kv_sh + sq.k_start * a.kv_st);
@@ -129,7 +148,7 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(AttentionArgs a, const 
       }
     }
   };
-  if (n_tiles > 0) fetch(0);
+  if (t_begin < t_end) fetch(t_begin);
 
   // ---- queries: B fragments
   bf16x8 qf[KS];
@@ -146,10 +165,10 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(AttentionArgs a, const 
     for (int e = 0; e < 16; ++e) o[i][e] = 0.0f;
   float m = -INFINITY, l = 0.0f;           // reference and this lane's part of the sum, base 2
 
-  for (int t = 0; t < n_tiles; ++t) {
+  for (int t = t_begin; t < t_end; ++t) {
     // the tile is in LDS (each wave waits for its own requests, the barrier for all), and everyone is done with the place of the next
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (t + 1 < n_tiles) fetch(t + 1);
+    if (t + 1 < t_end) fetch(t + 1);
     const int j0 = t * C::KEYS;
     if (j0 >= wave_most) continue;
     const char *ks = ring + (t % C::STAGES) * C::STAGE, *vs = ks + C::TILE;
@@ -249,9 +268,19 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(AttentionArgs a, const 
   // ---- normalise and write
   l = add_halves(l, l);
   const bool exists = first_row + wave * 32 + col < n_rows;
+  if (it.n_splits > 1) {                  // joined by join_kernel
+    const int64_t r = ((int64_t)blockIdx.x * a.splits + split) * ATT_ROWS + wave * 32 + col;
+    if (exists && half == 0) stats[r] = make_float2(m, l);
+#pragma unroll
+    for (int i = 0; i < VT; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        if (exists) *(float4 *)(part + r * D + i * 32 + e * 2 + half * 4) = make_float4(o[i][e], o[i][e + 1], o[i][e + 2], o[i][e + 3]);
+    return;
+  }
   if (exists && half == 0 && qi >= q_len - a.lse_rows)
     lse[((int64_t)sq.b * a.Hq + h * a.G + g) * a.lse_rows + (qi - (q_len - a.lse_rows))] =
-        l > 0.0f ? (m + fast_log2(l)) * 0.69314718055994531f : l == 0.0f ? -INFINITY : l;
+        row_lse(m, l);
   const float inv = seen > 0 ? 1.0f / l : 0.0f;
   char *op = out + (sq.b * a.o_sb + (int64_t)(h * a.G + g) * a.o_sh + (sq.q_start + qi) * a.o_st);
 #pragma unroll
@@ -272,17 +301,69 @@ __global__ __launch_bounds__(256, 2) void prefill_kernel(AttentionArgs a, const 
   }
 }
 
+// The rows of blocks that several workgroups shared: D / 4 threads a row, four channels each.
+constexpr int JOIN_THREADS = 256;
 template <int D, int DT>
-hipError_t launch_d(const AttentionPlan &plan, const void *q, const void *k, const void *v, void *out, float *lse, hipStream_t stream) {
-  hipLaunchKernelGGL((prefill_kernel<D, DT>), dim3((uint32_t)plan.items), dim3(256), 0, stream, plan.args, (const char *)q, (const char *)k, (const char *)v,
+__global__ __launch_bounds__(JOIN_THREADS) void join_kernel(AttentionArgs a, const float *__restrict__ part, const float2 *__restrict__ stats,
+                                                            char *__restrict__ out, float *__restrict__ lse) {
+  using C = Att<D, DT>;
+  constexpr int COLS = D / 4, ROWS = JOIN_THREADS / COLS, AHEAD = 4;
+  const Block it(a, blockIdx.x, C::KEYS);
+  const int r = blockIdx.y * ROWS + threadIdx.x / COLS, c = threadIdx.x % COLS * 4, row = it.block * ATT_ROWS + r;
+  if (it.n_splits == 1 || row >= it.n_rows) return;
+  const int64_t at = (int64_t)blockIdx.x * a.splits * ATT_ROWS + r;
+  const int last = it.n_splits - 1;
+  float m = -INFINITY, l = 0.0f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s0 = 0; s0 <= last; s0 += AHEAD) {
+    float2 ml[AHEAD];
+    float4 x[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int64_t from = at + (int64_t)min(s0 + u, last) * ATT_ROWS;
+      ml[u] = stats[from];
+      x[u] = *(const float4 *)(part + from * D + c);
+    }
+    float to = m;
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) to = fmaxf(to, ml[u].x);
+    const float ref = to == -INFINITY ? 0.0f : to, old = fast_exp2(m - ref);
+    m = to;
+    l *= old; o.x *= old; o.y *= old; o.z *= old; o.w *= old;
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const float w = s0 + u <= last ? fast_exp2(ml[u].x - ref) : 0.0f;
+      l = fmaf(ml[u].y, w, l);
+      o.x = fmaf(x[u].x, w, o.x); o.y = fmaf(x[u].y, w, o.y); o.z = fmaf(x[u].z, w, o.z); o.w = fmaf(x[u].w, w, o.w);
+    }
+  }
+  const int qi = it.query(row), g = row - qi * a.G, first = it.sq.q_len - a.lse_rows;
+  if (c == 0 && qi >= first)
+    lse[((int64_t)it.sq.b * a.Hq + it.h * a.G + g) * a.lse_rows + (qi - first)] = row_lse(m, l);
+  const float inv = it.sees(row) > 0 ? 1.0f / l : 0.0f;
+  char *op = out + (it.sq.b * a.o_sb + (int64_t)(it.h * a.G + g) * a.o_sh + (it.sq.q_start + qi) * a.o_st + c * C::ES);
+  if constexpr (DT == DT_F32) *(float4 *)op = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+  else *(uint2 *)op = make_uint2(pack_pair<DT>(o.x * inv, o.y * inv), pack_pair<DT>(o.z * inv, o.w * inv));
+}
+
+template <int D, int DT>
+hipError_t launch_d(const AttentionPlan &plan, const void *q, const void *k, const void *v, void *out, float *lse, void *ws, hipStream_t stream) {
+  const AttentionArgs &a = plan.args;
+  float *part = (float *)ws;
+  float2 *stats = (float2 *)((char *)ws + plan.stats_at);
+  hipLaunchKernelGGL((prefill_kernel<D, DT>), dim3((uint32_t)plan.items, (uint32_t)a.splits), dim3(Att<D, DT>::NT), 0, stream, a, (const char *)q,
+                     (const char *)k, (const char *)v, (char *)out, lse, part, stats);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.splits == 1) return e;
+  hipLaunchKernelGGL((join_kernel<D, DT>), dim3((uint32_t)plan.items, ATT_ROWS / (JOIN_THREADS / (D / 4))), dim3(JOIN_THREADS), 0, stream, a, part, stats,
                      (char *)out, lse);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_attention(const AttentionPlan &plan, const void *q, const void *k, const void *v, void *out, float *lse, void *, hipStream_t stream) {
-#define WKV_ATT_TYPE(DT) return plan.args.d == 128 ? launch_d<128, DT>(plan, q, k, v, out, lse, stream) : launch_d<64, DT>(plan, q, k, v, out, lse, stream)
+hipError_t launch_attention(const AttentionPlan &plan, const void *q, const void *k, const void *v, void *out, float *lse, void *ws, hipStream_t stream) {
+#define WKV_ATT_TYPE(DT) return plan.args.d == 128 ? launch_d<128, DT>(plan, q, k, v, out, lse, ws, stream) : launch_d<64, DT>(plan, q, k, v, out, lse, ws, stream)
   if (plan.args.dtype == WKV_BF16) WKV_ATT_TYPE(DT_BF16);
   if (plan.args.dtype == WKV_F16) WKV_ATT_TYPE(DT_F16);
   WKV_ATT_TYPE(DT_F32);

@@ -42,13 +42,21 @@ wkv_status check_workspace(const void *ws, size_t bytes, size_t needed) {
 }
 size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 
-// An angular frequency as turns per token modulo one, in units of 2^-64 turns.  (The division in 64 bits of mantissa: a position of
-// 2^31 leaves an error of 2^-33 turns of its frequency's 53 bits.)
+// An angular frequency as turns per token modulo one, in units of 2^-64 turns.  In integers, as 64 divisions of 80-bit floats take 3 us: a double is
+// m * 2^e, and 1 / (2 pi) is TURN * 2^-66 with 64 significant bits.  (A position of 2^31 leaves an error of 2^-33 turns of
+// the frequency's own 53 bits.)
 uint64_t turns_of(double inv_freq) {
-  const long double turns = (long double)inv_freq / 6.283185307179586476925286766559L;
-  const long double part = turns - floorl(turns);                // 0 <= part <= 1
-  const long double scaled = ldexpl(part, 64);
-  return scaled >= 18446744073709551615.0L ? 0 : (uint64_t)(scaled + 0.5L);
+  constexpr uint64_t TURN = 0xa2f9836e4e441529ull;
+  uint64_t bits;
+  std::memcpy(&bits, &inv_freq, 8);
+  const int exponent = (int)(bits >> 52 & 0x7ff);
+  const uint64_t mantissa = (bits & 0xfffffffffffffull) | (exponent ? 1ull << 52 : 0);
+  const int shift = 66 - 64 - ((exponent ? exponent : 1) - 1075);        // turns * 2^64 = mantissa * TURN * 2^-shift
+  const unsigned __int128 product = (unsigned __int128)mantissa * TURN;
+  uint64_t turns = 0;
+  if (shift <= 0) turns = shift > -64 ? (uint64_t)product << -shift : 0;
+  else if (shift < 128) turns = (uint64_t)(product >> shift) + (uint64_t)(product >> (shift - 1) & 1);
+  return bits >> 63 ? 0 - turns : turns;
 }
 
 }  // namespace
@@ -87,6 +95,32 @@ wkv_status plan_rope(const wkv_rope_shape *p, RopeArgs *a) {
   a->inverse = (p->flags & WKV_ROPE_INVERSE) ? 1 : 0;
   a->amplitude = p->amplitude == 0.0 ? 1.0f : (float)p->amplitude;
   return WKV_OK;
+}
+
+// Where the blocks alone do not fill the device, several workgroups share the key tiles of a block, `chunk` tiles each, and
+// a second launch joins their results.
+static void split_attention(AttentionPlan *plan) {
+  constexpr int64_t SLOTS = 512;        // workgroups that the device holds: two a compute unit
+  AttentionArgs &a = plan->args;
+  a.chunk = 0x7fffffff; a.splits = 1;
+  plan->stats_at = 0; plan->ws_bytes = 256;
+  if (plan->items == 0 || plan->items >= SLOTS) return;
+  const int32_t keys = att_tile_keys(a.dtype), least = a.dtype == WKV_F32 ? 2 : 4;
+  int64_t total = 0, most = 0;
+  for (int32_t i = 0; i < a.n_seqs; ++i)
+    for (int32_t block = 0; block < a.seq[i].blocks && a.seq[i].q_len > 0; ++block) {
+      const AttentionSeq &s = a.seq[i];
+      const int64_t last = std::min<int64_t>((int64_t)(block + 1) * ATT_ROWS, (int64_t)s.q_len * a.G) - 1;
+      const int64_t seen = std::min<int64_t>(std::max<int64_t>(last / a.G + s.k_len - s.q_len + 1, 0), s.k_len), tiles = ceil_div(seen, keys);
+      total += tiles * a.Hkv;
+      most = std::max(most, tiles);
+    }
+  const int64_t chunk = std::max<int64_t>(ceil_div(total, SLOTS), least), splits = ceil_div(most, chunk);
+  if (splits < 2) return;
+  a.chunk = (int32_t)ceil_div(most, splits); a.splits = (int32_t)ceil_div(most, a.chunk);
+  const size_t rows = (size_t)plan->items * a.splits * ATT_ROWS;
+  plan->stats_at = rows * a.d * sizeof(float);
+  plan->ws_bytes = round_up(plan->stats_at + rows * sizeof(float2));
 }
 
 wkv_status plan_attention(const wkv_attention_shape *p, AttentionPlan *plan) {
@@ -141,7 +175,7 @@ wkv_status plan_attention(const wkv_attention_shape *p, AttentionPlan *plan) {
   }
   plan->items = (int32_t)items;
   a.g_magic = division_magic(a.G);
-  plan->ws_bytes = 256;
+  split_attention(plan);
   return WKV_OK;
 }
 

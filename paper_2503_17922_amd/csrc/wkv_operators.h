@@ -41,11 +41,16 @@ struct AttentionArgs {
   uint32_t g_magic;                      // division_magic(G)
   float c1;                              // scale * log2(e)
   int64_t q_sb, q_sh, q_st, kv_sb, kv_sh, kv_st, o_sb, o_sh, o_st;      // bytes
+  int32_t chunk, splits;                 // key tiles of a workgroup, workgroups of a block with the most tiles (see plan_attention)
 };
+// (Keys of a tile: wkv_attention.hip has them as KEYS.)
+inline int32_t att_tile_keys(int32_t dtype) { return dtype == WKV_F32 ? 32 : 64; }
+// Partial results in the workspace, of blocks that more than one workgroup shares: outputs float [items][splits][ATT_ROWS][d], then
+// their references and sums float2 [items][splits][ATT_ROWS].
 struct AttentionPlan {
   AttentionArgs args;
   int32_t items;
-  size_t ws_bytes;
+  size_t stats_at, ws_bytes;
 };
 wkv_status plan_attention(const wkv_attention_shape *p, AttentionPlan *plan);
 hipError_t launch_attention(const AttentionPlan &plan, const void *q, const void *k, const void *v, void *out, float *lse, void *workspace,
