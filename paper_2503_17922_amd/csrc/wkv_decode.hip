@@ -130,9 +130,9 @@ __device__ __forceinline__ const float2 &part_stats(const DecodeShape &s, const 
   return *(const float2 *)((const char *)part + (s.stats_at + at * 8u));
 }
 
-// Where the logit of row j and head g is kept (WEIGHTS).
+// Where the logit of row j and head g is kept (WEIGHTS): blocks of 16 rows, [head][row] within, so that the block of a wave is one dense piece.
 __device__ __forceinline__ float *logit_at(const DecodeShape &s, const DecodeWeights &w, int bh, int g, int j) {
-  return w.logits + (((int64_t)bh * s.G + g) * ((int64_t)s.n_splits * s.chunk) + j);
+  return w.logits + (((int64_t)bh * ((int64_t)s.n_splits * s.chunk) + (j & ~15)) * s.G + g * 16 + (j & 15));
 }
 
 // Merge the per-wave states in LDS ([wave][head][D outputs, m, l]) and store the workgroup's
@@ -353,6 +353,8 @@ __global__ __launch_bounds__(NT, 3) void decode_partial_mfma_kernel(
   constexpr int KS = D / 32;                 // MFMA steps over the channels
   __shared__ __attribute__((aligned(16))) float o_s[WAVES][G][D];
   __shared__ float2 ml_s[WAVES][G];
+  constexpr int ROUND = PAIRS ? 24 * 4 / (G < 4 ? 4 : G) : 1;          // blocks whose logits a wave collects
+  __shared__ __attribute__((aligned(16))) float logit_s[WEIGHTS ? WAVES : 1][WEIGHTS ? ROUND : 1][G * 16];
 
   // (all arguments together, ahead of the row count that depends on one of them)
   asm volatile("" ::"s"(s.B), "s"(s.Hkv), "s"(s.heads_magic), "s"(s.kv_magic), "s"(s.chunk), "s"(s.capacity), "s"(s.c1), "s"(s.sb), "s"(s.sh), "s"(s.st),
@@ -415,6 +417,20 @@ __global__ __launch_bounds__(NT, 3) void decode_partial_mfma_kernel(
 #pragma unroll
     for (int t = 0; t < VT; ++t) x.v[t] = load_piece<(STREAM > 0)>(vr + va[t] + piece * 16);
   };
+  // WEIGHTS: a wave collects its logits in LDS, ROUND blocks at a time.  Stored as they come, they would be waited for with every round's rows (stores and
+  // loads are counted together), and in registers they cost a wave a SIMD: 64 sequences of 4128 rows 246 and 232 us a step, 200 so.  (Plain stores
+  // leave 34 MB to be written back behind the launch, 217; without any 178.)
+  int n_kept = 0;
+  auto store_logits = [&](int last_blk) __attribute__((always_inline)) {        // those of the last n_kept blocks, up to last_blk
+    __builtin_amdgcn_wave_barrier();
+    int first = threadIdx.x & 63;
+    asm volatile("" : "+v"(first));
+    for (int i = first; i < n_kept * (G * 4); i += 64) {
+      const int blk = last_blk - (n_kept - 1 - i / (G * 4)) * WAVES;
+      __builtin_nontemporal_store(*(const f32x4 *)&logit_s[wave][i / (G * 4)][i % (G * 4) * 4], (f32x4 *)(logit_at(s, w, bh, 0, c0 + blk * 16) + i % (G * 4) * 4));
+    }
+    n_kept = 0;
+  };
   auto attend = [&](const Block &x, int blk) __attribute__((always_inline)) {
     // scores of 16 rows x 16 (padded) heads
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -425,8 +441,12 @@ __global__ __launch_bounds__(NT, 3) void decode_partial_mfma_kernel(
     float sc[4], pr[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) sc[e] = r0 + e < cend ? acc[e] * s.c1 : -INFINITY;
-    // (a whole piece of four rows also past the end: ranges are multiples of 64 rows)
-    if (WEIGHTS && col < G) *(float4 *)logit_at(s, w, bh, col, r0) = make_float4(sc[0], sc[1], sc[2], sc[3]);
+    if (WEIGHTS) {                           // (four rows also past the end: ranges are multiples of 64)
+      int at = threadIdx.x;
+      asm volatile("" : "+v"(at));           // (nothing that follows from it stays in registers between blocks)
+      if ((at & 15) < G) *(f32x4 *)&logit_s[wave][n_kept][(at & 15) * 16 + (at >> 4 & 3) * 4] = (f32x4){sc[0], sc[1], sc[2], sc[3]};
+      ++n_kept;
+    }
     float mn = quads_max(fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3])));
     if (PAIRS) mn = fmaxf(m, mn);
     // -inf: every row so far has a logit of -inf (an infinite key, products that overflow) and weighs nothing
@@ -464,6 +484,7 @@ __global__ __launch_bounds__(NT, 3) void decode_partial_mfma_kernel(
       load_block(x, wave);
       __builtin_amdgcn_sched_barrier(0);       // the values too, before the scores wait for the keys
       attend(x, wave);
+      if (WEIGHTS) store_logits(wave);
     } else {
 #pragma unroll
       for (int i = 0; i < G * E; ++i) o[i] = 0.0f;
@@ -485,6 +506,7 @@ __global__ __launch_bounds__(NT, 3) void decode_partial_mfma_kernel(
         x = next;
       }
       __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0), reached by now but for rows requested past the end; else the compiler waits for the queries among the first requests
+      if (WEIGHTS && (n_kept > ROUND - 2 || c0 + (blk + WAVES) * 16 >= cend)) store_logits(blk);
     }
   }
 
@@ -538,7 +560,8 @@ __global__ __launch_bounds__(NT, 3) void decode_partial_mfma_kernel(
 // With few ranges one wave does it all and weighs them without LDS, a lane each (16 sequences of 500 rows 11.53 -> 11.28 us a layer; four
 // waves that each weigh up to 64 ranges for themselves, 9.55 -> 9.84 us for one sequence of 4128 rows: not so).
 // WEIGHTS: the workgroups from G on in y add up the attention weights of the cache's rows, each normalised for itself.
-constexpr int WEIGHT_ROWS = 4;        // rows of a thread at once
+constexpr int WEIGHT_ROWS = 4;        // rows of a thread at once (all heads' logits requested together, or the first ahead of the normalisers, are more code
+                                      // to fetch: one sequence of 4128 rows 4.1 -> 5.7 us)
 template <typename T, int D, int NT>
 __device__ __forceinline__ void add_weights(const DecodeShape &s, const T *q_new, const T *k_new, const float *part, const DecodeWeights &w,
                                             int bh, int b, int first_part, int n_parts) {

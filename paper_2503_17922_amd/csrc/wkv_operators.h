@@ -58,7 +58,7 @@ hipError_t launch_attention(const AttentionPlan &plan, const void *q, const void
 
 // ---- decode step with weights ---------------------------------------------------------------------
 // Behind the partial results in the workspace: the row counts of this step, int32 [B*Hkv], then the logits (base 2),
-// float [B*Hkv][G][n_splits * chunk].
+// float [B*Hkv][n_splits * chunk / 16][G][16].
 struct DecodeWeights {
   float *weights;
   int32_t *tok_idx;
