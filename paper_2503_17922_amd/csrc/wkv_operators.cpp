@@ -97,30 +97,59 @@ wkv_status plan_rope(const wkv_rope_shape *p, RopeArgs *a) {
   return WKV_OK;
 }
 
-// Where the blocks alone do not fill the device, several workgroups share the key tiles of a block, `chunk` tiles each, and
-// a second launch joins their results.
-static void split_attention(AttentionPlan *plan) {
-  constexpr int64_t SLOTS = 512;        // workgroups that the device holds: two a compute unit
-  AttentionArgs &a = plan->args;
-  a.chunk = 0x7fffffff; a.splits = 1;
-  plan->stats_at = 0; plan->ws_bytes = 256;
-  if (plan->items == 0 || plan->items >= SLOTS) return;
-  const int32_t keys = att_tile_keys(a.dtype), least = a.dtype == WKV_F32 ? 2 : 4;
-  int64_t total = 0, most = 0;
-  for (int32_t i = 0; i < a.n_seqs; ++i)
-    for (int32_t block = 0; block < a.seq[i].blocks && a.seq[i].q_len > 0; ++block) {
-      const AttentionSeq &s = a.seq[i];
-      const int64_t last = std::min<int64_t>((int64_t)(block + 1) * ATT_ROWS, (int64_t)s.q_len * a.G) - 1;
-      const int64_t seen = std::min<int64_t>(std::max<int64_t>(last / a.G + s.k_len - s.q_len + 1, 0), s.k_len), tiles = ceil_div(seen, keys);
-      total += tiles * a.Hkv;
-      most = std::max(most, tiles);
+// How the work is cut: blocks of 128 or 256 rows, and `splits` workgroups that share the key tiles of a block where the blocks alone do not fill the device (a
+// second launch joins their results).  By an estimate of the time in us, fitted to some forty shapes, of which it takes the best cut or one within a
+// few percent of it (a sixth at worst): a workgroup of 256 rows has a compute unit for itself, two of 128 share one and take twice as long; every workgroup has a
+// start, and every partial result is written and read.  us by blocks of 128 / 256 rows, 32q/8kv heads of 128 channels, bf16, each with its best number of
+// splits: 128 tokens 7.7 / 9.9, 1024 24.1 / 28.1, 2048 47.4 / 57.7, 4096 146 / 132, 200 tokens over 20000 86 / 84, 1024 over 20000 318 / 300; whole / cut
+// in its best number: one token over 20000 320 / 19.5, 512 tokens of 12q/2kv heads 14.3 / 12.6, 4096 of these 84 / 80, 2048 in fp32 278 / 315, 1024 139 / 89.
+struct AttentionCut {
+  int32_t rows, chunk, splits;
+};
+// (The key tiles of a sequence's blocks rise evenly from the first block's to the last one's, so sums over them need no loop.)
+static AttentionCut cut_attention(const wkv_attention_shape *p) {
+  const int64_t G = p->n_q_heads / p->n_kv_heads, Hkv = p->n_kv_heads;
+  const bool f32 = p->dtype == WKV_F32;
+  const int32_t keys = att_tile_keys(f32);
+  constexpr double UNITS = 256.0;               // compute units
+  constexpr int32_t WHOLE = 0x7fffffff;
+  AttentionCut best = {f32 ? ATT_ROWS_FEW : ATT_ROWS, WHOLE, 1};
+  double best_time = 1e300;
+  struct { double n, least, most; } blocks[WKV_MAX_BATCH];
+  for (const int32_t rows : {ATT_ROWS_FEW, ATT_ROWS}) {
+    if (f32 && rows != ATT_ROWS_FEW) continue;
+    const double tile = (p->head_dim == 128 ? 1.0 : 0.62) * (f32 ? 3.4 : rows == ATT_ROWS ? 1.75 : 1.15), start = rows == ATT_ROWS ? 5.0 : 4.0;
+    double n_blocks = 0, total = 0;
+    int64_t most = 0;
+    for (int32_t b = 0; b < p->batch; ++b) {
+      const int64_t q_len = p->q_len[b], k_len = p->k_len ? p->k_len[b] : q_len;
+      auto tiles = [&](int64_t last) { return ceil_div(std::min(std::max<int64_t>(last / G + k_len - q_len + 1, 0), k_len), (int64_t)keys); };
+      const int64_t top = q_len > 0 ? tiles(q_len * G - 1) : 0;
+      blocks[b] = {(double)(ceil_div(q_len * G, rows) * Hkv), q_len > 0 ? (double)tiles(std::min<int64_t>(rows, q_len * G) - 1) : 0.0, (double)top};
+      n_blocks += blocks[b].n;
+      total += blocks[b].n * (blocks[b].least + blocks[b].most) / 2;
+      most = std::max(most, top);
     }
-  const int64_t chunk = std::max<int64_t>(ceil_div(total, SLOTS), least), splits = ceil_div(most, chunk);
-  if (splits < 2) return;
-  a.chunk = (int32_t)ceil_div(most, splits); a.splits = (int32_t)ceil_div(most, a.chunk);
-  const size_t rows = (size_t)plan->items * a.splits * ATT_ROWS;
-  plan->stats_at = rows * a.d * sizeof(float);
-  plan->ws_bytes = round_up(plan->stats_at + rows * sizeof(float2));
+    for (const int32_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+      if (want > 1 && (want > most || n_blocks * want > 4096)) break;
+      const double chunk = want == 1 ? std::max<double>((double)most, 1) : (double)ceil_div(most, want);
+      double parts = 0, joined = 0, full = 0;             // workgroups, rows of partial results, workgroups with a whole chunk
+      for (int32_t b = 0; b < p->batch; ++b) {
+        const double n = blocks[b].n, lo = blocks[b].least, hi = blocks[b].most;
+        if (hi <= chunk) { parts += n; full += lo == hi && hi == chunk ? n : 0; continue; }
+        const double mean = (lo + hi) / 2 / chunk, cut = lo >= chunk ? 1.0 : (hi - chunk) / (hi - lo);     // share of the blocks that are cut
+        const double pieces = lo == hi ? std::ceil(mean) : mean + 0.5;
+        parts += n * pieces; joined += n * (cut * pieces) * std::min<double>(rows, (double)p->q_len[b] * (double)G); full += n * (lo == hi ? std::floor(mean) : std::max(mean - 0.5, 0.0));
+      }
+      double time = start + tile * std::max(chunk, total / UNITS) + 2.0 * parts / UNITS;
+      if (want > 1) {
+        if (rows == ATT_ROWS) time = std::max(time, start + tile * chunk * std::ceil(full / UNITS));      // (equal ones: whole rounds)
+        time += 5.0 + joined * p->head_dim * 4 * 2 / 4e6 + 0.35 * tile * chunk * std::min(std::max(parts / UNITS - 1.0, 0.0), 1.0);
+      }
+      if (time < best_time) { best_time = time; best = {rows, want == 1 ? WHOLE : (int32_t)chunk, want == 1 ? 1 : (int32_t)ceil_div(most, (int64_t)chunk)}; }
+    }
+  }
+  return best;
 }
 
 wkv_status plan_attention(const wkv_attention_shape *p, AttentionPlan *plan) {
@@ -163,19 +192,32 @@ wkv_status plan_attention(const wkv_attention_shape *p, AttentionPlan *plan) {
     if ((int64_t)s.q_len * a.G > ATT_MAX || s.k_len > ATT_MAX || ((int64_t)s.q_len * a.G + ATT_ROWS) * a.G > 0xffffffffll) {
       set_error("sequence %d has too many rows or keys; split the call", b); return WKV_ERR_UNSUPPORTED;
     }
-    // (a sequence without rows has a block for the normalisers of rows that do not exist)
-    s.blocks = (int32_t)std::max<int64_t>(ceil_div((int64_t)s.q_len * a.G, ATT_ROWS), p->lse_rows > 0 ? 1 : 0);
+    plan->most_rows = (int32_t)std::max<int64_t>(plan->most_rows, (int64_t)s.q_len * a.G);
   }
+  const AttentionCut cut = cut_attention(p);
+  plan->rows = cut.rows;
+  plan->most_rows = std::min(plan->most_rows, cut.rows);
+  // (a sequence without rows has a block for the normalisers of rows that do not exist)
+  for (int32_t b = 0; b < p->batch; ++b)
+    a.seq[b].blocks = (int32_t)std::max<int64_t>(ceil_div((int64_t)a.seq[b].q_len * a.G, plan->rows), p->lse_rows > 0 ? 1 : 0);
   std::sort(a.seq, a.seq + p->batch, [](const AttentionSeq &x, const AttentionSeq &y) { return x.blocks != y.blocks ? x.blocks > y.blocks : x.b < y.b; });
   int64_t items = 0;
   for (int32_t i = 0; i < WKV_MAX_BATCH; ++i) {
     if (i < p->batch) items += (int64_t)(a.seq[i].blocks - (i + 1 < p->batch ? a.seq[i + 1].blocks : 0)) * (i + 1) * a.Hkv;
-    if (items > 1 << 23) { set_error("more than 2^23 blocks of %d rows; split the call", ATT_ROWS); return WKV_ERR_UNSUPPORTED; }      // (launch grid limit)
+    if (items > 1 << 23) { set_error("more than 2^23 blocks of %d rows; split the call", plan->rows); return WKV_ERR_UNSUPPORTED; }      // (launch grid limit)
     a.ends[i] = (int32_t)items;
   }
   plan->items = (int32_t)items;
   a.g_magic = division_magic(a.G);
-  split_attention(plan);
+  a.chunk = cut.chunk; a.splits = cut.splits;
+  a.fold_from = plan->rows == ATT_ROWS_FEW && a.splits == 1 && items > 256 && items <= 512 && items % 8 == 0 ? 256 : 0x7fffffff;
+  a.fold_parts = items % 8 == 0 ? 0 : 0x7fffffff;
+  plan->ws_bytes = 256;
+  if (a.splits > 1) {
+    const size_t rows = (size_t)items * a.splits * plan->rows;
+    plan->stats_at = rows * a.d * sizeof(float);
+    plan->ws_bytes = round_up(plan->stats_at + rows * sizeof(float2));
+  }
   return WKV_OK;
 }
 

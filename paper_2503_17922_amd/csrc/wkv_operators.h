@@ -24,12 +24,14 @@ wkv_status plan_rope(const wkv_rope_shape *p, RopeArgs *a);
 hipError_t launch_rope(const RopeArgs &a, hipStream_t stream);
 
 // ---- attention over a prompt --------------------------------------------------------------------
-// A work item is ATT_ROWS rows of one (sequence, KV head): row r is query r / G of its query head r % G, so that the heads of a
-// KV head share the key tiles.
-constexpr int32_t ATT_ROWS = 128;
+// A work item is a block of 128 or 256 rows of one (sequence, KV head): row r is query r / G of its query head r % G, so that the heads of
+// a KV head share the key tiles.  (Both sides of the launch go by these: a kernel that took other blocks or tiles than the plan has would
+// write past the workspace.)
+constexpr int32_t ATT_ROWS = 256, ATT_ROWS_FEW = 128;
+constexpr int32_t att_tile_keys(bool f32) { return f32 ? 32 : 64; }      // keys of a tile
 constexpr int32_t ATT_MAX = 1 << 30;     // most rows of a (sequence, KV head), and most keys
 struct AttentionSeq {
-  int32_t b, q_len, k_len, blocks;       // blocks of ATT_ROWS rows
+  int32_t b, q_len, k_len, blocks;       // blocks of AttentionPlan::rows rows
   int64_t q_start, k_start;
 };
 struct AttentionArgs {
@@ -42,14 +44,13 @@ struct AttentionArgs {
   float c1;                              // scale * log2(e)
   int64_t q_sb, q_sh, q_st, kv_sb, kv_sh, kv_st, o_sb, o_sh, o_st;      // bytes
   int32_t chunk, splits;                 // key tiles of a workgroup, workgroups of a block with the most tiles (see plan_attention)
+  int32_t fold_from, fold_parts;         // from these workgroups on the items go the other way round (wkv_attention.hip, item_of)
 };
-// (Keys of a tile: wkv_attention.hip has them as KEYS.)
-inline int32_t att_tile_keys(int32_t dtype) { return dtype == WKV_F32 ? 32 : 64; }
-// Partial results in the workspace, of blocks that more than one workgroup shares: outputs float [items][splits][ATT_ROWS][d], then
-// their references and sums float2 [items][splits][ATT_ROWS].
+// Partial results in the workspace, of blocks that more than one workgroup shares: outputs float [items][splits][rows][d], then
+// their references and sums float2 [items][splits][rows].
 struct AttentionPlan {
   AttentionArgs args;
-  int32_t items;
+  int32_t items, rows, most_rows;        // blocks, their rows, and the most that any of them has
   size_t stats_at, ws_bytes;
 };
 wkv_status plan_attention(const wkv_attention_shape *p, AttentionPlan *plan);
