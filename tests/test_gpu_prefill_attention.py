@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2503_17922_amd as W
+from tests.test_attention_cut import SHAPES
 
 pytestmark = pytest.mark.gpu
 
@@ -172,6 +173,12 @@ def test_one_key_is_its_value(device):
 @pytest.mark.parametrize("Hq,H,n", [(32, 8, 2000), (28, 4, 1501), (8, 8, 4097)])
 def test_long_prompts(device, Hq, H, n):
     run(device, [n], [n], Hq, H, 128, W.WKV_BF16, lse_rows=32)
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "-".join(str(x) for x in s[:4]) + f"-{len(s[4])}x{s[4][0]}")
+def test_every_cut_of_the_work(device, shape):
+    Hq, H, d, dtype, q_len, k_len = shape
+    run(device, q_len, k_len, Hq, H, d, dtype, lse_rows=7, seed=len(q_len))
 
 
 def test_many_sequences(device):
