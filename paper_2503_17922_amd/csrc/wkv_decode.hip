@@ -93,6 +93,12 @@ __device__ __forceinline__ float row_lanes_sum(float x) {
   return x;
 }
 
+__device__ __forceinline__ float row_lanes_max8(float x) {
+  x = fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0xB1, 0xF, 0xF, false)));  // quad_perm [1,0,3,2]
+  x = fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x4E, 0xF, 0xF, false)));  // quad_perm [2,3,0,1]
+  return fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x141, 0xF, 0xF, false)));      // row_half_mirror
+}
+
 // Sum and maximum over the wave, in every lane: DPP steps inside rows of 16 lanes, then two permlane swaps.
 __device__ __forceinline__ float wave_sum(float x) { return quads_sum(row16_sum(x)); }
 __device__ __forceinline__ float wave_max(float x) {
@@ -568,22 +574,44 @@ __device__ __forceinline__ void add_weights(const DecodeShape &s, const T *q_new
   __shared__ float top[8], over_sum[8], logit_new[8];
   const int n = w.counts[bh], tid = threadIdx.x, lane = tid & 63;
   if (n < 0 || n >= s.capacity || (int64_t)first_part * (NT * WEIGHT_ROWS) > n) return;
-  for (int g = tid >> 6; g < s.G; g += NT / 64) {
+  auto keep = [&](int g, float logit, float mm, float sum) __attribute__((always_inline)) {
+    const bool none = mm == -INFINITY;              // no row weighs anything
+    top[g] = none ? 0.0f : mm;
+    over_sum[g] = none ? 0.0f : 1.0f / sum;
+    logit_new[g] = logit;
+  };
+  if constexpr (NT == 64) {                         // a wave and few ranges: all heads at once, eight lanes each
+    using P = Piece<T>;
+    const int g = lane >> 3, sub = lane & 7, gc = min(g, s.G - 1);
     float dot = 0.0f, m = -INFINITY, l = 0.0f;
-    for (int sp = lane; sp < s.n_splits; sp += 64) {
-      const float2 ml = part_stats(s, part, part_index(s, bh, sp, g));
+    for (int sp = sub; sp < s.n_splits; sp += 8) {
+      const float2 ml = part_stats(s, part, part_index(s, bh, sp, gc));
       merge_stats(m, l, ml.x, ml.y);
     }
 #pragma unroll
-    for (int c = 0; c < D; c += 64)
-      dot = fmaf(Piece<T>::value(q_new + ((int64_t)bh * s.G + g) * D + c + lane), Piece<T>::value(k_new + (int64_t)bh * D + c + lane), dot);
-    const float logit = wave_sum(dot) * s.c1, mm = fmaxf(wave_max(m), logit);
-    const float sum = wave_sum(m == -INFINITY ? 0.0f : l * fast_exp2(m - mm)) + fast_exp2(logit - mm);
-    if (lane == 0) {
-      const bool none = mm == -INFINITY;              // no row weighs anything
-      top[g] = none ? 0.0f : mm;
-      over_sum[g] = none ? 0.0f : 1.0f / sum;
-      logit_new[g] = logit;
+    for (int c = 0; c < D; c += 8 * P::E) {
+      float qf[P::E], kf[P::E];
+      P::unpack(*(const uint4 *)(q_new + ((int64_t)bh * s.G + gc) * D + c + sub * P::E), qf);
+      P::unpack(*(const uint4 *)(k_new + (int64_t)bh * D + c + sub * P::E), kf);
+#pragma unroll
+      for (int i = 0; i < P::E; ++i) dot = fmaf(qf[i], kf[i], dot);
+    }
+    const float logit = row_lanes_sum<8>(dot) * s.c1, mm = fmaxf(row_lanes_max8(m), logit);
+    const float sum = row_lanes_sum<8>(m == -INFINITY ? 0.0f : l * fast_exp2(m - mm)) + fast_exp2(logit - mm);
+    if (sub == 0 && g < s.G) keep(g, logit, mm, sum);
+  } else {
+    for (int g = tid >> 6; g < s.G; g += NT / 64) {
+      float dot = 0.0f, m = -INFINITY, l = 0.0f;
+      for (int sp = lane; sp < s.n_splits; sp += 64) {
+        const float2 ml = part_stats(s, part, part_index(s, bh, sp, g));
+        merge_stats(m, l, ml.x, ml.y);
+      }
+#pragma unroll
+      for (int c = 0; c < D; c += 64)
+        dot = fmaf(Piece<T>::value(q_new + ((int64_t)bh * s.G + g) * D + c + lane), Piece<T>::value(k_new + (int64_t)bh * D + c + lane), dot);
+      const float logit = wave_sum(dot) * s.c1, mm = fmaxf(wave_max(m), logit);
+      const float sum = wave_sum(m == -INFINITY ? 0.0f : l * fast_exp2(m - mm)) + fast_exp2(logit - mm);
+      if (lane == 0) keep(g, logit, mm, sum);
     }
   }
   __syncthreads();
