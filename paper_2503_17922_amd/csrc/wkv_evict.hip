@@ -7,7 +7,7 @@
 //                   place, and one row too many costs one row's copy instead of half a cache's.
 //   move kernel     copies the rows of every layer's keys and values.
 // The selection reads 8 bytes a row and is a chain of scans, bound by their latency (4097 rows: 20.6 us with the weights read anew in every
-// step and fixed digits, 11.2 so); the copies by memory, in pieces of a row here and there (5 TB/s).
+// step and fixed digits, 9.9 so); the copies by memory, in pieces of a row here and there (5 TB/s).
 #include <algorithm>
 
 #include "wkv_device.h"
@@ -47,80 +47,23 @@ struct EvictLds {
   uint32_t bin, above, count;
 };
 
-// Rows are dealt to the waves in ranges, in row order, a lane every 64th of its wave's range.  HELD: a thread keeps its weights and
-// positions in registers (ranges of up to HELD * 64 rows); 0: they are read again in every step.
-template <int HELD>
-__device__ __forceinline__ void evict_rows(const EvictArgs &a, EvictLds &lds, int32_t *holes, int n, int stay, float *w, int32_t *tok, int2 *mv, int &n_moves) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int per_wave = ((n + EV_WAVES - 1) / EV_WAVES + 63) / 64 * 64;
-  const int from = min(wave * per_wave, n), to = min(from + per_wave, n), iters = (to - from + 63) / 64;
-  const uint64_t below = ((uint64_t)1 << lane) - 1;
-  constexpr int N = HELD ? HELD : 1;
-  float own_w[N];
-  int32_t own_tok[N];
-  if constexpr (HELD > 0) {
-#pragma unroll
-    for (int i = 0; i < HELD; ++i) { const int j = min(from + i * 64 + lane, n - 1); own_w[i] = w[j]; own_tok[i] = tok[j]; }
-  }
-  // f(i, row, is a row, its weight, its position) for every row of the thread, all lanes of a wave together
-  auto each = [&](auto &&f) __attribute__((always_inline)) {
-    if constexpr (HELD > 0) {
-#pragma unroll
-      for (int i = 0; i < HELD; ++i)
-        if (i < iters) f(i, from + i * 64 + lane, from + i * 64 + lane < to, own_w[i], own_tok[i]);
-    } else {
-      for (int i = 0; i < iters; ++i) {
-        const int j = from + i * 64 + lane, at = min(j, n - 1);
-        f(i, j, j < to, w[at], tok[at]);
-      }
-    }
-  };
-
-  // ---- 1. the last position; rows within `recent` of it are protected
-  uint32_t last = 0;
-  each([&](int, int, bool in, float, int32_t t) { last = max(last, in ? (uint32_t)t ^ 0x80000000u : 0u); });      // signed order to unsigned
-  last = wave_largest(last);
-  if (lane == 0) lds.waves[0][wave] = last;
-  for (int i = tid; i < EV_BINS; i += EV_THREADS) lds.bins[i] = 0;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < EV_WAVES; ++i) last = max(last, lds.waves[0][i]);
-  const int64_t old = (int64_t)(int32_t)(last ^ 0x80000000u) - a.recent;        // positions up to this one are not protected
-
-  // ---- 2. how many are, and the range of the weights of either kind
-  uint32_t fresh = 0, least[2] = {0xffffffffu, 0xffffffffu}, most[2] = {0, 0};
-  each([&](int, int, bool in, float x, int32_t t) {
-    const bool f = t > old;
-    const uint32_t key = weight_key(x);
-    fresh += __builtin_popcountll(__ballot(in && f));
-#pragma unroll
-    for (int c = 0; c < 2; ++c)
-      if (in && f == (c == 1)) { least[c] = min(least[c], key); most[c] = max(most[c], key); }
-  });
-#pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    const uint32_t lo = ~wave_largest(~least[c]), hi = wave_largest(most[c]);
-    if (lane == 0) { lds.waves[1 + 2 * c][wave] = lo; lds.waves[2 + 2 * c][wave] = hi; }
-  }
-  uint32_t n_fresh;
-  before_this_wave(fresh, lds.waves[5], wave, n_fresh);
-  // Protected rows come first; where they do not all fit, they alone are selected from, by weight.
-  const bool crowded = (int)n_fresh > stay;
-  uint32_t remaining = crowded ? stay : stay - n_fresh;                  // of the rows that are selected from
-  uint32_t lo = 0xffffffffu, hi = 0;
-#pragma unroll
-  for (int i = 0; i < EV_WAVES; ++i) { lo = min(lo, lds.waves[crowded ? 3 : 1][i]); hi = max(hi, lds.waves[crowded ? 4 : 2][i]); }
-
-  // ---- 3. the key of the last row that stays, by digits of the range that the keys span (digits from the top of the word would put nearly
-  // all weights into a few bins and serialise the counters); until what still fits is a whole bin or a bin is one key wide
-  uint32_t bound = 0xffffffffu, take_eq = 0;           // keys above `bound` stay, and the first take_eq rows that have it
+// The key of the last row that stays, by digits of the range [lo, hi] that the keys span (digits from the top of the word would put nearly
+// all weights into a few bins and serialise the counters); until what still fits is a whole bin or a bin is one key wide.  count(lo, hi, shift): adds up
+// the rows with keys from lo to hi in bins, (key - lo) >> shift.  `counted`: that has been done for the first range.
+struct Bound {
+  uint32_t key, take_eq;                    // keys above it stay, and the first take_eq rows that have it
+};
+__device__ __forceinline__ int digit_shift(uint32_t lo, uint32_t hi) { return max(32 - __clz((int)((hi - lo) | 1u)) - 11, 0); }
+template <class F>
+__device__ __forceinline__ Bound last_that_stays(EvictLds &lds, uint32_t remaining, uint32_t lo, uint32_t hi, bool counted, F &&count) {
+  const int tid = threadIdx.x, wave = tid >> 6;
   while (remaining > 0) {
-    const int bits = 32 - __clz((int)((hi - lo) | 1u)), shift = max(bits - 11, 0);
-    each([&](int, int, bool in, float x, int32_t t) {
-      const uint32_t key = weight_key(x);
-      if (in && (t > old) == crowded && key >= lo && key <= hi) atomicAdd(&lds.bins[(key - lo) >> shift], 1u);
-    });
-    __syncthreads();
+    const int shift = digit_shift(lo, hi);
+    if (!counted) {
+      count(lo, hi, shift);
+      __syncthreads();
+    }
+    counted = false;
     const int b0 = EV_BINS - 1 - 2 * tid;              // two bins a thread, the largest digit first
     const uint32_t c0 = lds.bins[b0], c1 = lds.bins[b0 - 1], upto = wave_sums(c0 + c1);
     uint32_t all, above = before_this_wave(last_lane(upto), lds.waves[6], wave, all) + upto - c0 - c1;
@@ -131,88 +74,221 @@ __device__ __forceinline__ void evict_rows(const EvictArgs &a, EvictLds &lds, in
     __syncthreads();
     remaining -= lds.above;
     const uint32_t bin_lo = lo + (lds.bin << shift);
-    if (shift == 0) { bound = bin_lo; take_eq = remaining; break; }
-    if (lds.count == remaining) { bound = bin_lo - 1; break; }           // (bin_lo > 0: 0 is no weight's key)
+    if (shift == 0) return {bin_lo, remaining};
+    if (lds.count == remaining) return {bin_lo - 1, 0};           // (bin_lo > 0: 0 is no weight's key)
     hi = bin_lo + min((1u << shift) - 1u, hi - bin_lo);
     lo = bin_lo;
   }
-
-  // ---- 4. dropped rows below `stay`, and kept rows from there on: their numbers, then their ranks
-  uint32_t rank = 0, all;
-  auto keeps = [&](bool in, float x, int32_t t) __attribute__((always_inline)) {
-    const bool f = t > old;
-    const uint32_t key = weight_key(x);
-    bool kept = in && (f != crowded ? f : key > bound);
-    if (take_eq > 0) {                                 // (uniform)
-      const uint64_t same = __ballot(in && f == crowded && key == bound);
-      kept |= (same >> lane & 1) && rank + __builtin_popcountll(same & below) < take_eq;
-      rank += __builtin_popcountll(same);
-    }
-    return kept;
-  };
-  uint32_t equal_before = 0;
-  if (take_eq > 0) {
-    uint32_t equal = 0;
-    each([&](int, int, bool in, float x, int32_t t) { equal += __builtin_popcountll(__ballot(in && (t > old) == crowded && weight_key(x) == bound)); });
-    equal_before = before_this_wave(equal, lds.waves[7], wave, all);
-  }
-  rank = equal_before;
-  uint32_t n_holes = 0, n_late = 0;
-  each([&](int, int j, bool in, float x, int32_t t) {
-    const bool kept = keeps(in, x, t);
-    n_holes += __builtin_popcountll(__ballot(in && !kept && j < stay));
-    n_late += __builtin_popcountll(__ballot(kept && j >= stay));
-  });
-  uint32_t hole = before_this_wave(n_holes, lds.waves[0], wave, all), late = before_this_wave(n_late, lds.waves[1], wave, all);
-  n_moves = (int)all;
-  rank = equal_before;
-  each([&](int, int j, bool in, float x, int32_t t) {
-    const uint64_t open = __ballot(in && !keeps(in, x, t) && j < stay);
-    if (open >> lane & 1) {
-      const uint32_t r = hole + __builtin_popcountll(open & below);
-      if (HELD) holes[r] = j; else mv[r].y = j;
-    }
-    hole += __builtin_popcountll(open);
-  });
-  __syncthreads();
-  rank = equal_before;
-  each([&](int, int j, bool in, float x, int32_t t) {
-    const uint64_t comes = __ballot(keeps(in, x, t) && j >= stay);
-    if (comes >> lane & 1) {
-      const uint32_t r = late + __builtin_popcountll(comes & below);
-      const int32_t dst = HELD ? holes[r] : mv[r].y;
-      mv[r] = make_int2(j, dst);
-      if (HELD) { w[dst] = x; tok[dst] = t; }
-    }
-    late += __builtin_popcountll(comes);
-  });
-  if constexpr (HELD == 0) {                           // (nobody reads the rows below `stay` any more)
-    __syncthreads();
-    for (int i = tid; i < n_moves; i += EV_THREADS) {
-      const int2 m = mv[i];
-      w[m.y] = w[m.x];
-      tok[m.y] = tok[m.x];
-    }
-  }
+  return {0xfffffffeu, 0};                             // only the rows that are not selected from
 }
 
-// HELD * 1024 rows or fewer (LONG: where there are more, their weights are read in every step).
-template <int HELD, bool LONG>
+// Keys of rows that always stay (protected ones, where they all fit) and that never do (the others, where not).
+constexpr uint32_t ALWAYS = 0xffffffffu, NEVER = 0u;
+
+// Rows are dealt to the waves in ranges, in row order, a lane every 64th of its wave's range.  A bit a turn tells which of a thread's rows stay.
+struct Range {
+  int from, to, turns;
+  __device__ __forceinline__ Range(int n, int wave) {
+    const int per_wave = ((n + EV_WAVES - 1) / EV_WAVES + 63) / 64 * 64;
+    from = min(wave * per_wave, n); to = min(from + per_wave, n); turns = (to - from + 63) / 64;
+  }
+};
+
+// Up to ROWS rows: their keys lie in LDS.  (In registers, a thread's rows unrolled, the code is four times as long, and a launch fetches it anew: 4097 rows
+// 11.2 us, 9.9 so.)
+template <int ROWS>
+__device__ __forceinline__ int evict_rows(const EvictArgs &a, EvictLds &lds, uint32_t *keys, int32_t *toks, int n, int stay, float *w, int32_t *tok, int2 *mv) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Range r(n, wave);
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  constexpr int AHEAD = 4;
+
+  // ---- 1. the last position, whose `recent` rows are protected, and the range of the weights
+  uint32_t last = 0, lo = 0xffffffffu, hi = 0;
+  for (int i = 0; i < r.turns; i += AHEAD) {
+    float x[AHEAD];
+    int32_t t[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) { const int j = min(r.from + (i + u) * 64 + lane, r.to - 1); x[u] = w[j]; t[u] = tok[j]; }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {                  // (past the end: the last row again)
+      const int j = min(r.from + (i + u) * 64 + lane, r.to - 1);
+      const uint32_t key = weight_key(x[u]);
+      keys[j] = key; toks[j] = t[u];
+      last = max(last, (uint32_t)t[u] ^ 0x80000000u);               // signed order to unsigned
+      lo = min(lo, key); hi = max(hi, key);
+    }
+  }
+  last = wave_largest(last); lo = ~wave_largest(~lo); hi = wave_largest(hi);
+  if (lane == 0) { lds.waves[0][wave] = last; lds.waves[1][wave] = lo; lds.waves[2][wave] = hi; }
+  for (int i = tid; i < EV_BINS; i += EV_THREADS) lds.bins[i] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < EV_WAVES; ++i) { last = max(last, lds.waves[0][i]); lo = min(lo, lds.waves[1][i]); hi = max(hi, lds.waves[2][i]); }
+  const int64_t old = (int64_t)(int32_t)(last ^ 0x80000000u) - a.recent;        // positions up to this one are not protected
+
+  // ---- 2. the protected rows, and the first digit of the others
+  uint32_t fresh = 0, n_fresh;
+  const int shift = digit_shift(lo, hi);
+  for (int i = 0; i < r.turns; ++i) {
+    const int j = r.from + i * 64 + lane;
+    const bool in = j < r.to, f = in && toks[j] > old;
+    fresh += __builtin_popcountll(__ballot(f));
+    if (f) keys[j] = ALWAYS;
+    else if (in) atomicAdd(&lds.bins[(keys[j] - lo) >> shift], 1u);
+  }
+  before_this_wave(fresh, lds.waves[3], wave, n_fresh);
+  const bool crowded = (int)n_fresh > stay;
+  if (crowded) {                             // they do not all fit: they alone are selected from, by weight
+    for (int i = tid; i < EV_BINS; i += EV_THREADS) lds.bins[i] = 0;
+    __syncthreads();
+    for (int j = r.from + lane; j < r.to; j += 64) {
+      const uint32_t key = toks[j] > old ? weight_key(w[j]) : NEVER;
+      keys[j] = key;
+      if (key != NEVER) atomicAdd(&lds.bins[(key - lo) >> shift], 1u);
+    }
+    __syncthreads();
+  }
+  const Bound bound = last_that_stays(lds, crowded ? stay : stay - n_fresh, lo, hi, true, [&](uint32_t lo, uint32_t hi, int shift) {
+    for (int j = r.from + lane; j < r.to; j += 64)
+      if (keys[j] >= lo && keys[j] <= hi) atomicAdd(&lds.bins[(keys[j] - lo) >> shift], 1u);
+  });
+
+  // ---- 3. which rows stay; dropped ones below `stay` and kept ones from there on: their numbers, then their ranks
+  uint32_t stays = 0, rank = 0, n_holes = 0, n_late = 0, all;
+  if (bound.take_eq > 0) {
+    uint32_t equal = 0;
+    for (int i = 0; i < r.turns; ++i) {
+      const int j = r.from + i * 64 + lane;
+      equal += __builtin_popcountll(__ballot(j < r.to && keys[j] == bound.key));
+    }
+    rank = before_this_wave(equal, lds.waves[4], wave, all);
+  }
+  static_assert(ROWS <= 32 * EV_THREADS, "a bit a turn");
+  for (int i = 0; i < r.turns; ++i) {
+    const int j = r.from + i * 64 + lane;
+    const bool in = j < r.to;
+    const uint32_t key = in ? keys[j] : NEVER;
+    bool kept = key > bound.key;
+    if (bound.take_eq > 0) {                           // (uniform)
+      const uint64_t same = __ballot(in && key == bound.key);
+      kept |= (same >> lane & 1) && rank + __builtin_popcountll(same & below) < bound.take_eq;
+      rank += __builtin_popcountll(same);
+    }
+    stays |= (uint32_t)kept << i;
+    n_holes += __builtin_popcountll(__ballot(in && !kept && j < stay));
+    n_late += __builtin_popcountll(__ballot(kept && j >= stay));
+  }
+  if (lane == 0) lds.waves[5][wave] = n_late;
+  uint32_t hole = before_this_wave(n_holes, lds.waves[7], wave, all), late = 0;
+#pragma unroll
+  for (int i = 0; i < EV_WAVES; ++i) late += i < wave ? lds.waves[5][i] : 0u;
+  int32_t *holes = toks;                     // (nobody looks at the positions any more)
+  for (int i = 0; i < r.turns; ++i) {
+    const int j = r.from + i * 64 + lane;
+    const uint64_t open = __ballot(j < min(r.to, stay) && !(stays >> i & 1));
+    if (open >> lane & 1) holes[hole + __builtin_popcountll(open & below)] = j;
+    hole += __builtin_popcountll(open);
+  }
+  __syncthreads();
+  for (int i = 0; i < r.turns; ++i) {
+    const int j = r.from + i * 64 + lane;
+    const uint64_t comes = __ballot(j >= stay && (stays >> i & 1));
+    if (comes >> lane & 1) {
+      const int at = late + __builtin_popcountll(comes & below), to = holes[at];
+      mv[at] = make_int2(j, to);
+      w[to] = w[j];
+      tok[to] = tok[j];
+    }
+    late += __builtin_popcountll(comes);
+  }
+  return (int)all;
+}
+
+// Any number of rows: the same steps, with the weights read in each.
+__device__ __forceinline__ int evict_long(const EvictArgs &a, EvictLds &lds, int n, int stay, float *w, int32_t *tok, int2 *mv) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Range r(n, wave);
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  uint32_t last = 0, all;
+  for (int j = r.from + lane; j < r.to; j += 64) last = max(last, (uint32_t)tok[j] ^ 0x80000000u);
+  last = wave_largest(last);
+  if (lane == 0) lds.waves[0][wave] = last;
+  for (int i = tid; i < EV_BINS; i += EV_THREADS) lds.bins[i] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < EV_WAVES; ++i) last = max(last, lds.waves[0][i]);
+  const int64_t old = (int64_t)(int32_t)(last ^ 0x80000000u) - a.recent;
+  uint32_t fresh = 0, n_fresh;
+  for (int i = 0; i < r.turns; ++i) {
+    const int j = r.from + i * 64 + lane;
+    fresh += __builtin_popcountll(__ballot(j < r.to && tok[j] > old));
+  }
+  before_this_wave(fresh, lds.waves[3], wave, n_fresh);
+  const bool crowded = (int)n_fresh > stay;
+  auto key_of = [&](int j) __attribute__((always_inline)) {
+    const bool f = tok[j] > old;
+    return f != crowded ? (f ? ALWAYS : NEVER) : weight_key(w[j]);
+  };
+  const Bound bound = last_that_stays(lds, crowded ? stay : stay - n_fresh, 1u, 0xfffffffeu, false, [&](uint32_t lo, uint32_t hi, int shift) {
+    for (int j = r.from + lane; j < r.to; j += 64) {
+      const uint32_t key = key_of(j);
+      if (key >= lo && key <= hi) atomicAdd(&lds.bins[(key - lo) >> shift], 1u);
+    }
+  });
+  uint32_t equal = 0;
+  for (int i = 0; i < r.turns; ++i) {
+    const int j = r.from + i * 64 + lane;
+    equal += __builtin_popcountll(__ballot(j < r.to && key_of(j) == bound.key));
+  }
+  const uint32_t equal_before = before_this_wave(equal, lds.waves[4], wave, all);
+  auto walk = [&](uint32_t &holes, uint32_t &late, bool emit) __attribute__((always_inline)) {
+    uint32_t rank = equal_before;
+    for (int i = 0; i < r.turns; ++i) {
+      const int j = r.from + i * 64 + lane;
+      const bool in = j < r.to;
+      const uint32_t key = in ? key_of(j) : NEVER;
+      const uint64_t same = __ballot(in && key == bound.key);
+      const bool kept = in && (key > bound.key || ((same >> lane & 1) && rank + __builtin_popcountll(same & below) < bound.take_eq));
+      rank += __builtin_popcountll(same);
+      const uint64_t open = __ballot(in && !kept && j < stay), comes = __ballot(kept && j >= stay);
+      if (emit && (open >> lane & 1)) mv[holes + __builtin_popcountll(open & below)].y = j;
+      if (emit && (comes >> lane & 1)) mv[late + __builtin_popcountll(comes & below)].x = j;
+      holes += __builtin_popcountll(open);
+      late += __builtin_popcountll(comes);
+    }
+  };
+  uint32_t holes = 0, late = 0, n_moves;
+  walk(holes, late, false);
+  holes = before_this_wave(holes, lds.waves[5], wave, n_moves);
+  late = before_this_wave(late, lds.waves[7], wave, all);
+  walk(holes, late, true);
+  __syncthreads();
+  for (int i = tid; i < (int)n_moves; i += EV_THREADS) {
+    const int2 m = mv[i];
+    w[m.y] = w[m.x];
+    tok[m.y] = tok[m.x];
+  }
+  return (int)n_moves;
+}
+
+// LONG: caches may have more than ROWS rows.
+template <int ROWS, bool LONG>
 __global__ __launch_bounds__(EV_THREADS) void evict_select_kernel(EvictArgs a, float *weights, int32_t *tok_idx, int32_t *n_valid,
                                                                   const int32_t *__restrict__ keep, int32_t *__restrict__ counts,
                                                                   int2 *__restrict__ moves) {
   __shared__ EvictLds lds;
-  __shared__ int32_t holes[HELD * EV_THREADS / 2];     // at most min(stay, n - stay)
+  __shared__ uint32_t keys[ROWS];
+  __shared__ int32_t toks[ROWS];
   const int row = blockIdx.x, n = n_valid[row], stay = keep[row];
   int n_moves = 0;
   if (stay >= 0 && n <= a.capacity && n > stay) {
     float *w = weights + (int64_t)row * a.capacity;
     int32_t *tok = tok_idx + (int64_t)row * a.capacity;
     int2 *mv = moves + (int64_t)row * a.max_moves;
-    if (!LONG || n <= HELD * EV_THREADS) evict_rows<HELD>(a, lds, holes, n, stay, w, tok, mv, n_moves);
-    else if constexpr (LONG) evict_rows<0>(a, lds, holes, n, stay, w, tok, mv, n_moves);
-    __syncthreads();                       // (every thread has read the count)
-    if (threadIdx.x == 0) n_valid[row] = stay;
+    if (!LONG || n <= ROWS) n_moves = evict_rows<ROWS>(a, lds, keys, toks, n, stay, w, tok, mv);
+    else n_moves = evict_long(a, lds, n, stay, w, tok, mv);
+    if (threadIdx.x == 0) n_valid[row] = stay;         // (every thread has read it: there was a synchronisation since)
   }
   if (threadIdx.x == 0) counts[row] = n_moves;
 }
@@ -254,11 +330,10 @@ __global__ __launch_bounds__(MOVE_THREADS) void evict_move_kernel(EvictArgs a, E
 
 hipError_t launch_evict(const EvictArgs &a, const EvictLayers &layers, int32_t n_layers, float *weights, int32_t *tok_idx, int32_t *n_valid,
                         const int32_t *keep, int32_t *counts, int2 *moves, hipStream_t stream) {
-#define WKV_SELECT(HELD, LONG) \
-  hipLaunchKernelGGL((evict_select_kernel<HELD, LONG>), dim3(a.rows), dim3(EV_THREADS), 0, stream, a, weights, tok_idx, n_valid, keep, counts, moves)
-  if (a.capacity <= 2 * EV_THREADS) WKV_SELECT(2, false);
-  else if (a.capacity <= 5 * EV_THREADS) WKV_SELECT(5, false);
-  else WKV_SELECT(12, true);
+#define WKV_SELECT(ROWS, LONG) \
+  hipLaunchKernelGGL((evict_select_kernel<ROWS, LONG>), dim3(a.rows), dim3(EV_THREADS), 0, stream, a, weights, tok_idx, n_valid, keep, counts, moves)
+  if (a.capacity <= 6144) WKV_SELECT(6144, false);          // (two workgroups a compute unit)
+  else WKV_SELECT(16384, true);
 #undef WKV_SELECT
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

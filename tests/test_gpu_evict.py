@@ -108,6 +108,15 @@ def test_equal_weights_go_by_the_lower_row(device, levels):
     State(device, [3000, 1500], 1111, 20, cap=3000, weights=w, seed=2).check()
 
 
+@pytest.mark.parametrize("n", [6145, 16384, 16385, 20000])
+@pytest.mark.parametrize("keep,recent", [(100, 30), (5000, 32), (6000, 6100), (0, 5), (6100, 0)])
+def test_long_caches_with_ties_and_many_protected_rows(device, n, keep, recent):
+    g = torch.Generator(device=device).manual_seed(n)
+    w = torch.randint(0, 50, (1, 2, n), device=device, generator=g).float()
+    w[0, 1, ::7] = math.nan
+    State(device, [n], keep, recent, d=64, layers=1, cap=n, weights=w, tok=torch.arange(n, device=device, dtype=torch.int32).repeat(1, 2, 1)).check()
+
+
 def test_every_kind_of_weight(device):
     g = torch.Generator(device=device).manual_seed(8)
     special = torch.tensor([math.nan, -math.nan, math.inf, -math.inf, 0.0, -0.0, 1e-45, -1e-45, 3.4e38, -3.4e38, 1.0, -1.0], device=device)
