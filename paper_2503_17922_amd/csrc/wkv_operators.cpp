@@ -165,6 +165,7 @@ wkv_status plan_attention(const wkv_attention_shape *p, AttentionPlan *plan) {
   if (p->head_dim != 64 && p->head_dim != 128) { set_error("head_dim %d is not supported (64 or 128)", p->head_dim); return WKV_ERR_UNSUPPORTED; }
   if (!(p->scale >= 0.0f) || std::isinf(p->scale)) return invalid("scale must be finite and >= 0 (0 selects 1/sqrt(head_dim))");
   if (p->lse_rows < 0) return invalid("lse_rows must be >= 0");
+  if ((int64_t)p->lse_rows * (p->n_q_heads / p->n_kv_heads) > ATT_MAX) { set_error("lse_rows %d is not supported", p->lse_rows); return WKV_ERR_UNSUPPORTED; }
   if (p->flags != 0) { set_error("unknown bits in flags (0x%x)", p->flags); return WKV_ERR_INVALID_ARG; }
   if (!good_strides(p->dtype, p->head_dim, p->q_stride_b, p->q_stride_h, p->q_stride_t, "q") ||
       !good_strides(p->dtype, p->head_dim, p->kv_stride_b, p->kv_stride_h, p->kv_stride_t, "K and V") ||

@@ -102,7 +102,7 @@ def attention(fields=None, q=FAKE, k=OTHER, v=C.c_void_p(3 << 20), out=C.c_void_
 SHAPES = [
     (dict(q_len=[]), INVALID), (dict(q_len=[1] * 65), UNSUPPORTED), (dict(n_q_heads=9), INVALID), (dict(n_kv_heads=0), INVALID), (dict(dtype=9), INVALID),
     (dict(head_dim=80), UNSUPPORTED), (dict(scale=-1.0), INVALID), (dict(scale=math.nan), INVALID), (dict(scale=math.inf), INVALID),
-    (dict(lse_rows=-1), INVALID), (dict(flags=1), INVALID), (dict(q_len=[-1, 5]), INVALID), (dict(k_len=[3, -2]), INVALID),
+    (dict(lse_rows=-1), INVALID), (dict(lse_rows=(1 << 28) + 1), UNSUPPORTED), (dict(flags=1), INVALID), (dict(q_len=[-1, 5]), INVALID), (dict(k_len=[3, -2]), INVALID),
     (dict(q_start=[0, -1]), INVALID), (dict(k_start=[-7, 0]), INVALID), (dict(q_strides=(0, 128, 100)), INVALID), (dict(kv_strides=(0, 64, 128)), INVALID),
     (dict(out_strides=(0, 128, 132)), INVALID), (dict(kv_strides=(0, 128, 1 << 25)), UNSUPPORTED), (dict(q_len=[2 ** 31 - 1, 1], q_strides=(0, 128, 128)), UNSUPPORTED),
     (dict(q_len=[1, 1], k_len=[2 ** 31 - 1, 1], kv_strides=(0, 128, 128)), UNSUPPORTED),
