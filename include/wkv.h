@@ -418,8 +418,9 @@ typedef struct {
 /*
  *   positions     device int32 [batch, n_tokens], contiguous; a row whose position is negative (padding) is left as it is
  *   q_in, k_in    device; e.g. the heads of one fused projection, by their strides
- *   q_out, k_out  device; may be the inputs themselves, with the same strides (in place).  Otherwise no output may
- *                 overlap an input or the other output.
+ *   q_out, k_out  device; may be the inputs themselves, with the same strides (in place).  Otherwise no row of an output may
+ *                 overlap a row of an input or of the other output, and in any case none another row of its own tensor.
+ * Tensors are 16-byte aligned, strides multiples of 16 bytes.  No workspace; calls on different streams may overlap in time.
  * Computed in fp32, rounded once.
  */
 wkv_status wkv_rope(const wkv_rope_shape *shape, const int32_t *positions, const void *q_in, void *q_out,
@@ -454,6 +455,8 @@ wkv_status wkv_rope_frequencies(int32_t rotary_dim, double theta, int32_t scalin
  * Tensor layouts (strides in ELEMENTS; the head_dim axis always has stride 1):
  *   q, out  [batch, n_q_heads,  rows, head_dim]   row i of sequence b lies at  b * stride_b + (q_start[b] + i) * stride_t
  *   K, V    [batch, n_kv_heads, rows, head_dim]   likewise with k_start[b]; V has K's strides
+ * Tensors are 16-byte aligned, strides multiples of 16 bytes; 64 tokens of K are less than 2 GiB apart (kv_stride_t).  A sequence has at
+ * most 2^30 keys and 2^30 rows of all query heads of a KV head together.
  * Padded batches and caches leave the starts NULL (0).  Packed sequences, one after the other in [rows, heads, head_dim],
  * have stride_b = 0 and their first rows in q_start and k_start.  Rows of no sequence are neither read nor written.
  */
@@ -475,13 +478,13 @@ typedef struct {
   int64_t out_stride_b, out_stride_h, out_stride_t;
 } wkv_attention_shape;
 
-/* Bytes of 256-byte-aligned device workspace wkv_prefill_attention needs; 0 for an invalid shape.  Its contents on entry are
- * irrelevant and on return unspecified; calls that may overlap in time need workspaces of their own. */
+/* Bytes of 256-byte-aligned device workspace wkv_prefill_attention needs for exactly these lengths (shorter ones can need more); 0 for an
+ * invalid shape.  Its contents on entry are irrelevant and on return unspecified; calls that may overlap in time need workspaces of their own. */
 size_t wkv_attention_workspace_bytes(const wkv_attention_shape *shape);
 
 /*
  *   q, k, v    device, layouts above.  Keys and values of the k_len rows must be finite; other rows may hold anything.
- *   out        device, layout above; must not overlap the inputs
+ *   out        device, layout above; must not overlap the inputs, nor a row another row
  *   lse_out    device float32 [batch, n_q_heads, lse_rows] (contiguous), or NULL with lse_rows = 0: entry r belongs to row
  *              q_len[b] - lse_rows + r, -inf where there is no such row.  With lse_rows = w_obs it is the lse_obs
  *              that wkv_score and wkv_compress_groups take.
@@ -500,7 +503,10 @@ wkv_status wkv_prefill_attention(const wkv_attention_shape *shape, const void *q
  *              scores of Eq. 2 at the retained positions
  *   tok_idx    device int32 [batch, n_kv_heads, capacity], contiguous, or NULL: token position of every cache row
  *   position   device int32 [batch], or NULL with tok_idx: position of the new token
- * Everything else as at wkv_decode_step, with a workspace of wkv_decode_weighted_workspace_bytes.  A (b, h) that cannot take the new row leaves its
+ * A step sets the new row's weight and adds to the others, so each array of weights belongs to one layer: layers that share their row counts have
+ * an array each, or one of them decides for all (the others take wkv_decode_step).
+ * Everything else as at wkv_decode_step, with a 256-byte-aligned workspace of wkv_decode_weighted_workspace_bytes (contents on entry
+ * irrelevant; calls that may overlap in time need workspaces of their own) and capacity <= 2^30.  A (b, h) that cannot take the new row leaves its
  * weights and positions as they are, too; where no row of a head weighs anything (all logits -inf), its weights count as 0.
  */
 size_t wkv_decode_weighted_workspace_bytes(const wkv_decode_shape *shape);
@@ -515,7 +521,7 @@ wkv_status wkv_decode_step_weighted(const wkv_decode_shape *shape, const void *q
  * lower row (a weight of NaN is less than any other).  Kept rows below keep stay where they are; the r-th kept row from there on
  * (ascending) moves into the r-th row below that is dropped, with its weight and position.  The rows of a cut cache are therefore in no order of
  * position, which attention over them does not depend on; tok_idx tells it.
- *   shape                the caches' shape; n_q_heads, scale and flags are not used
+ *   shape                the caches' shape, capacity <= 2^30; n_q_heads, scale and flags are not used (but must be valid)
  *   n_layers             1 .. WKV_MAX_LAYERS
  *   k_caches, v_caches   host arrays [n_layers] of device pointers; in place
  *   weights, tok_idx     device float32, int32 [batch, n_kv_heads, capacity], contiguous; in place
@@ -523,6 +529,7 @@ wkv_status wkv_decode_step_weighted(const wkv_decode_shape *shape, const void *q
  *   keep                 device int32 [batch, n_kv_heads]; negative: the (b, h) is left as it is
  *   recent               >= 0
  * A (b, h) whose n_valid is not in 0 .. capacity is left as it is.  Rows from the new count on hold what they held.
+ * Workspace: 256-byte aligned, contents on entry irrelevant; calls that may overlap in time need workspaces of their own.
  */
 size_t wkv_evict_workspace_bytes(const wkv_decode_shape *shape);
 wkv_status wkv_cache_evict(const wkv_decode_shape *shape, int32_t n_layers, void *const *k_caches, void *const *v_caches,
