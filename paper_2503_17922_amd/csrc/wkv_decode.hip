@@ -38,6 +38,7 @@ static __device__ __align__(256) unsigned char scratch[WKV_DECODE_STATIC_SCRATCH
 
 constexpr int DEC_THREADS = 256;
 constexpr int DEC_WAVES = DEC_THREADS / 64;
+constexpr int WHOLE_THREADS = 512, WHOLE_FLOATS = 20224;      // logits in LDS: two workgroups a compute unit, 80 KB each
 constexpr int WIDE_THREADS = 512;   // where a range is a block for each of eight waves (see launch_partial_g)
 constexpr int DEC_U = 4;            // row tiles per wave batch (loads in flight: 2 * DEC_U per lane)
 
@@ -347,20 +348,105 @@ template <int N, class F>
 __device__ __forceinline__ void static_for(F &&f) {
   if constexpr (N > 0) { static_for<N - 1>(f); f(std::integral_constant<int, N - 1>{}); }
 }
+// The end of a step whose rows one workgroup took (WHOLE): the new row, the weights from the logits in `logits`, the merge of the waves there.
+template <int D, int G, typename T, int NT, class F>
+__device__ __forceinline__ void finish_whole(const DecodeShape &s, const DecodeWeights &w, const uint16_t *q_new, uint16_t *k_cache, uint16_t *v_cache,
+                                             int bh, int b, int h, int n, float m, float l, float *logits, float2 (*ml_s)[G], F &&share_outputs) {
+  using P = Piece<T>;
+  constexpr int WAVES = NT / 64, E = P::E, LPK = D / E, AT_ONCE = 8;
+  static_assert(G <= WAVES, "a wave a head");
+  __shared__ float new_s[G];
+  __shared__ float2 head_s[G];               // what a head's logits lie above, one over their sum
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const T *k_new = (const T *)w.k_new + (int64_t)bh * D, *v_new = (const T *)w.v_new + (int64_t)bh * D;
+  // what comes from memory, together
+  const bool appends = tid < 2 * LPK;
+  uint4 row_piece = make_uint4(0, 0, 0, 0);
+  if (appends) row_piece = *(const uint4 *)((tid < LPK ? k_new : v_new) + tid % LPK * E);
+  float *const weights = w.weights + (int64_t)bh * s.capacity;
+  float old[AT_ONCE], dot = 0.0f;
+#pragma unroll
+  for (int i = 0; i < AT_ONCE; ++i) old[i] = weights[min(i * NT + tid, n)];
+  if (wave < G)
+#pragma unroll
+    for (int c = 0; c < D; c += 64) dot = fmaf(P::value((const T *)q_new + ((int64_t)bh * G + wave) * D + c + lane), P::value(k_new + c + lane), dot);
+  dot = wave_sum(dot) * s.c1;
+  if (wave < G && lane == 0) new_s[wave] = dot;
+  if (lane < G) ml_s[wave][lane] = make_float2(m, l);
+  __syncthreads();
+  auto total = [&](int g, float &mm, float &sum) __attribute__((always_inline)) {
+    mm = new_s[g];
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) mm = fmaxf(mm, ml_s[i][g].x);
+    sum = fast_exp2(new_s[g] - mm);
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) sum = fmaf(ml_s[i][g].y, fast_exp2(ml_s[i][g].x - mm), sum);
+  };
+  if (tid < G) {
+    float mm, sum;
+    total(tid, mm, sum);
+    const bool none = mm == -INFINITY;       // no row weighs anything
+    head_s[tid] = make_float2(none ? 0.0f : mm, none ? 0.0f : 1.0f / sum);
+  }
+  __syncthreads();
+  for (int r0 = 0; r0 <= n; r0 += AT_ONCE * NT) {
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int j = r0 + i * NT + tid;
+      float sum = 0.0f;
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const float x = j < n ? logits[(j & ~15) * G + g * 16 + (j & 15)] : new_s[g];
+        sum = fmaf(fast_exp2(x - head_s[g].x), head_s[g].y, sum);
+      }
+      if (j <= n) weights[j] = j < n ? old[i] + sum : sum;
+    }
+    if (r0 + AT_ONCE * NT <= n)
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) old[i] = weights[min(r0 + (AT_ONCE + i) * NT + tid, n)];
+  }
+  if (appends) *(uint4 *)((tid < LPK ? k_cache : v_cache) + ((int64_t)b * s.sb + (int64_t)h * s.sh + (int64_t)n * s.st + tid % LPK * E)) = row_piece;
+  if (tid == 0) {
+    if (w.tok_idx) w.tok_idx[(int64_t)bh * s.capacity + n] = w.position[b];
+    if (!s.keep_count) w.n_valid[bh] = n + 1;             // (everyone has read it)
+  }
+  __syncthreads();                           // (the logits are done with)
+  share_outputs();
+  __syncthreads();
+  for (int i = tid; i < G * (D / 4); i += NT) {
+    const int g = i / (D / 4), c = i % (D / 4) * 4;
+    float mm, sum;
+    total(g, mm, sum);
+    const float w_new = fast_exp2(new_s[g] - mm);
+    float4 o;
+    o.x = w_new * P::value(v_new + c); o.y = w_new * P::value(v_new + c + 1); o.z = w_new * P::value(v_new + c + 2); o.w = w_new * P::value(v_new + c + 3);
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) {
+      const float a = fast_exp2(ml_s[k][g].x - mm);
+      const float4 x = *(const float4 *)&logits[(k * G + g) * D + c];
+      o.x = fmaf(x.x, a, o.x); o.y = fmaf(x.y, a, o.y); o.z = fmaf(x.z, a, o.z); o.w = fmaf(x.w, a, o.w);
+    }
+    float *const to = w.out + ((int64_t)bh * G + g) * D + c;          // (aligned to a float alone)
+    to[0] = o.x / sum; to[1] = o.y / sum; to[2] = o.z / sum; to[3] = o.w / sum;
+  }
+}
+
 // STREAM: 0 plain loads, 1 values stream, 2 keys too (see launch_partial_g).
-template <int D, int G, bool F16, int STREAM, int NT, bool WEIGHTS>
-__global__ __launch_bounds__(NT, 3) void decode_partial_mfma_kernel(
+// WHOLE (with WEIGHTS): the whole step for a (sequence, KV head) by one workgroup, whose logits stay in LDS until its rows are through.
+template <int D, int G, bool F16, int STREAM, int NT, bool WEIGHTS, bool WHOLE = false>
+__global__ __launch_bounds__(NT, WHOLE ? 4 : 3) void decode_partial_mfma_kernel(
     DecodeShape s, const uint16_t *__restrict__ q_new, const uint16_t *k_cache,
     const uint16_t *v_cache, const int32_t *__restrict__ n_valid, float *__restrict__ part, DecodeWeights w) {
   constexpr int E = 8, WAVES = NT / 64;
-  constexpr bool PAIRS = WAVES == DEC_WAVES;
+  constexpr bool PAIRS = WHOLE || WAVES == DEC_WAVES;
   constexpr int LPK = D / E;                 // lanes per row (value side): 16 or 8
   constexpr int VT = D / 32;                 // value loads per block of 16 rows: rows of a quad / rows it reads at once
   constexpr int KS = D / 32;                 // MFMA steps over the channels
-  __shared__ __attribute__((aligned(16))) float o_s[WAVES][G][D];
+  __shared__ __attribute__((aligned(16))) float state_s[WHOLE ? WHOLE_FLOATS : WAVES * G * D];       // WHOLE: the logits [block][head][row] before
+  float (*const o_s)[G][D] = (float (*)[G][D])state_s;
   __shared__ float2 ml_s[WAVES][G];
-  constexpr int ROUND = PAIRS ? 24 * 4 / (G < 4 ? 4 : G) : 1;          // blocks whose logits a wave collects
-  __shared__ __attribute__((aligned(16))) float logit_s[WEIGHTS ? WAVES : 1][WEIGHTS ? ROUND : 1][G * 16];
+  constexpr int ROUND = WHOLE ? 1 : PAIRS ? 24 * 4 / (G < 4 ? 4 : G) : 1;          // blocks whose logits a wave collects
+  __shared__ __attribute__((aligned(16))) float logit_s[WEIGHTS && !WHOLE ? WAVES : 1][WEIGHTS ? ROUND : 1][G * 16];
 
   // (all arguments together, ahead of the row count that depends on one of them)
   asm volatile("" ::"s"(s.B), "s"(s.Hkv), "s"(s.heads_magic), "s"(s.kv_magic), "s"(s.chunk), "s"(s.capacity), "s"(s.c1), "s"(s.sb), "s"(s.sh), "s"(s.st),
@@ -377,9 +463,16 @@ __global__ __launch_bounds__(NT, 3) void decode_partial_mfma_kernel(
     __builtin_amdgcn_sched_barrier(0);       // (all that while the row count is under way)
     asm volatile("" ::"s"(kc), "s"(vc));
   }
-  const int n = item.n, c0 = split * s.chunk, cend = min(c0 + s.chunk, n < s.capacity ? n : 0);
-  if (WEIGHTS && split == 0 && threadIdx.x == 0) w.counts[bh] = n;
-  if (nothing_to_do<G>(s, bh, split, n, c0, cend, part)) return;
+  const int n = item.n, c0 = WHOLE ? 0 : split * s.chunk, cend = min(WHOLE ? n : c0 + s.chunk, n < s.capacity ? n : 0);
+  if constexpr (WHOLE) {
+    if (n < 0 || n >= s.capacity) {
+      for (int i = threadIdx.x; i < G * D; i += NT) w.out[(int64_t)bh * (G * D) + i] = __uint_as_float(0x7fc00000u);
+      return;
+    }
+  } else {
+    if (WEIGHTS && split == 0 && threadIdx.x == 0) w.counts[bh] = n;
+    if (nothing_to_do<G>(s, bh, split, n, c0, cend, part)) return;
+  }
 
   // query rows as B fragments: lane (head col, quad) holds channels 32*ks + 8*quad .. +7; columns past the
   // last head repeat it and are not used
@@ -424,8 +517,8 @@ __global__ __launch_bounds__(NT, 3) void decode_partial_mfma_kernel(
     for (int t = 0; t < VT; ++t) x.v[t] = load_piece<(STREAM > 0)>(vr + va[t] + piece * 16);
   };
   // WEIGHTS: a wave collects its logits in LDS, ROUND blocks at a time.  Stored as they come, they would be waited for with every round's rows (stores and
-  // loads are counted together), and in registers they cost a wave a SIMD: 64 sequences of 4128 rows 246 and 232 us a step, 200 so.  (Plain stores
-  // leave 34 MB to be written back behind the launch, 217; without any 178.)
+  // loads are counted together), and in registers they cost a wave a SIMD: 64 sequences of 4128 rows 246 and 232 us a step, 203 so.  (Plain stores
+  // leave 34 MB to be written back behind the launch, 217; without any 178: launch_whole.)
   int n_kept = 0;
   auto store_logits = [&](int last_blk) __attribute__((always_inline)) {        // those of the last n_kept blocks, up to last_blk
     __builtin_amdgcn_wave_barrier();
@@ -450,8 +543,10 @@ __global__ __launch_bounds__(NT, 3) void decode_partial_mfma_kernel(
     if (WEIGHTS) {                           // (four rows also past the end: ranges are multiples of 64)
       int at = threadIdx.x;
       asm volatile("" : "+v"(at));           // (nothing that follows from it stays in registers between blocks)
-      if ((at & 15) < G) *(f32x4 *)&logit_s[wave][n_kept][(at & 15) * 16 + (at >> 4 & 3) * 4] = (f32x4){sc[0], sc[1], sc[2], sc[3]};
-      ++n_kept;
+      const int to = (at & 15) * 16 + (at >> 4 & 3) * 4;
+      float *const block = WHOLE ? state_s + blk * (G * 16) : logit_s[WHOLE ? 0 : wave][n_kept];
+      if ((at & 15) < G) *(f32x4 *)&block[to] = (f32x4){sc[0], sc[1], sc[2], sc[3]};
+      n_kept += WHOLE ? 0 : 1;
     }
     float mn = quads_max(fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3])));
     if (PAIRS) mn = fmaxf(m, mn);
@@ -512,7 +607,7 @@ __global__ __launch_bounds__(NT, 3) void decode_partial_mfma_kernel(
         x = next;
       }
       __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0), reached by now but for rows requested past the end; else the compiler waits for the queries among the first requests
-      if (WEIGHTS && (n_kept > ROUND - 2 || c0 + (blk + WAVES) * 16 >= cend)) store_logits(blk);
+      if (WEIGHTS && !WHOLE && (n_kept > ROUND - 2 || c0 + (blk + WAVES) * 16 >= cend)) store_logits(blk);
     }
   }
 
@@ -528,13 +623,20 @@ __global__ __launch_bounds__(NT, 3) void decode_partial_mfma_kernel(
       o[i] += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, o[i]), 0x128, 0xF, 0xF, false));   // row_ror:8
   }
   l = quads_sum(l);
-  if (sub == 0) {
+  auto share_outputs = [&]() __attribute__((always_inline)) {
+    if (sub == 0) {
 #pragma unroll
-    for (int i = 0; i < N / 4; i += 2) {
-      const int at = quad * (N / 4) + i;         // value `at` is channel at % 8 of head at / 8; pairs never cross a head
-      *(float2 *)&o_s[wave][at / E][piece * E + at % E] = make_float2(o[i], o[i + 1]);
+      for (int i = 0; i < N / 4; i += 2) {
+        const int at = quad * (N / 4) + i;       // value `at` is channel at % 8 of head at / 8; pairs never cross a head
+        *(float2 *)&o_s[wave][at / E][piece * E + at % E] = make_float2(o[i], o[i + 1]);
+      }
     }
+  };
+  if constexpr (WHOLE) {
+    finish_whole<D, G, std::conditional_t<F16, half_t, uint16_t>, NT>(s, w, q_new, (uint16_t *)k_cache, (uint16_t *)v_cache, bh, b, h, n, m, l, state_s, ml_s, share_outputs);
+    return;
   }
+  share_outputs();
   if (lane < G) ml_s[wave][lane] = make_float2(m, l);        // lane = head (quad 0)
   __syncthreads();
 
@@ -827,10 +929,42 @@ static void launch_partial_g(const DecodeShape &s, dim3 grid, const void *q, con
 #undef WKV_PARTIAL
 }
 
+// Whether one workgroup takes all rows of a (sequence, KV head), and the launch that does: where they fill the compute units, one or two to each, and
+// the logits of full caches fit into half a unit's LDS.  The logits make no trip through memory then (34 MB written among the rows' reads cost the launch of 64
+// sequences 20 of 187 us), and there is no second launch; but nobody takes over a long cache's rows.  us by ranges / so, 32q/8kv heads of 128
+// channels, 4128 rows, three sets of caches in turn: 16 sequences 60 / 66, 20 71 / 68, 28 97 / 81, 32 107 / 92, 34 118 / 133, 44 148 / 145, 52 168 / 160,
+// 64 203 / 179, 128 411 / 361; 1000 rows, 32 33.0 / 26.7, 52 48 / 42, 64 59 / 48; mixed, 500 to 4000 rows, 24 57 / 59, 28 68 / 65, 32 83 / 72, 48 92 / 103,
+// 52 113 / 105, 64 133 / 119; one of 4500 rows among 63 of 300 46 / 60; 64 channels, 64q/8kv, 2000 rows, 32 40 / 34, 64 70 / 54.  With 128 channels and more than four
+// heads the registers of two workgroups a unit do not suffice.  Values stream, keys do not (both: 64 of 4128 rows 180, mixed ones 127).
+template <int D, int G, bool F16>
+static bool launch_whole(const DecodeShape &s, const void *q, const void *kc, const void *vc, int32_t *n_valid, const DecodeWeights &w, hipStream_t stream) {
+  if constexpr (D == 128 && G > 4) {
+    return false;
+  } else {
+    constexpr int UNITS = 256;
+    const int rows = s.B * s.Hkv;
+    if (!((rows >= UNITS * 7 / 8 && rows <= UNITS) || rows >= UNITS * 13 / 8)) return false;
+    if (((int64_t)s.capacity + 15) / 16 * 16 * G > WHOLE_FLOATS) return false;
+    hipLaunchKernelGGL((decode_partial_mfma_kernel<D, G, F16, 1, WHOLE_THREADS, true, true>), dim3(rows), dim3(WHOLE_THREADS), 0, stream, s,
+                       (const uint16_t *)q, (const uint16_t *)kc, (const uint16_t *)vc, n_valid, (float *)nullptr, w);
+    return true;
+  }
+}
+
 template <typename T, int D, bool WEIGHTS>
 static hipError_t launch_decode_t(const DecodeShape &s, const void *q, const void *kn, const void *vn, void *kc, void *vc,
                                   int32_t *n_valid, float *out, float *part, const DecodeWeights &w, hipStream_t stream) {
   const dim3 grid(s.B * s.Hkv, s.n_splits);
+  if constexpr (WEIGHTS && sizeof(T) == 2) {
+    DecodeWeights all = w;
+    all.k_new = kn; all.v_new = vn; all.n_valid = n_valid; all.out = out;
+#define WKV_WHOLE(GG) case GG: if (launch_whole<D, GG, !__is_same(T, uint16_t)>(s, q, kc, vc, n_valid, all, stream)) return hipGetLastError(); break;
+    switch (s.G) {
+      WKV_WHOLE(1) WKV_WHOLE(2) WKV_WHOLE(3) WKV_WHOLE(4) WKV_WHOLE(5) WKV_WHOLE(6) WKV_WHOLE(7) WKV_WHOLE(8)
+      default: break;
+    }
+#undef WKV_WHOLE
+  }
 #define WKV_DEC_CASE(GG) \
   case GG: launch_partial_g<T, D, GG, WEIGHTS>(s, grid, q, kc, vc, n_valid, part, w, stream); break;
   switch (s.G) {

@@ -66,6 +66,9 @@ struct DecodeWeights {
   const int32_t *position;
   int32_t *counts;
   float *logits;
+  const void *k_new, *v_new;             // and these where one launch does the whole step
+  int32_t *n_valid;
+  float *out;
 };
 size_t decode_weighted_layout(const DecodeShape &s, size_t partial_bytes, size_t *counts_at, size_t *logits_at);
 hipError_t launch_decode_weighted(const DecodeShape &s, const void *q_new, const void *k_new, const void *v_new, void *k_cache,

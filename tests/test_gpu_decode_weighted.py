@@ -145,3 +145,88 @@ def test_captured_and_replayed(device):
         c.step()
         for x, y in zip(("kc", "vc", "n", "weights", "tok", "out"), got):
             assert torch.equal(getattr(c, x), y), x
+
+
+def check_whole(c, with_tok=True):
+    """A step whose rows one workgroup takes (as many (sequence, KV head) rows as compute units, or twice that): outputs, weights, caches and counts in 64 bits."""
+    before = {x: getattr(c, x).clone(memory_format=torch.preserve_format) for x in ("kc", "vc", "n", "weights", "tok")}
+    c.step(**({} if with_tok else dict(tok=None, at=None)))
+    B, H, cap = c.weights.shape
+    G, d = c.q.shape[1] // H, c.q.shape[2]
+    assert B * H >= 224 and cap <= 20224 // G // 16 * 16
+    out = c.out.view(B, H, G, d)
+    want = {x: before[x] for x in before}
+    for b in range(B):
+        for h in range(H):
+            n = int(before["n"][b, h])
+            if not 0 <= n < cap:
+                assert torch.isnan(out[b, h]).all()
+                continue
+            want["kc"][b, h, n], want["vc"][b, h, n], want["n"][b, h] = c.kn[b, h], c.vn[b, h], n + 1
+            if with_tok:
+                want["tok"][b, h, n] = c.at[b]
+            q, k, v = c.q[b, h * G:(h + 1) * G].double(), want["kc"][b, h, :n + 1].double(), want["vc"][b, h, :n + 1].double()
+            p = torch.softmax(q @ k.t() * c.scale, -1)
+            # a logit is off by (d + 4) 2^-24 scale |q| |k|, a probability by twice that and, with the sum of n terms and the exponents, (n + 16) 2^-24; sums of
+            # products by as much again, the additions to a weight by half a step of the result each
+            delta = (d + 4) * 2.0 ** -24 * c.scale * q.norm(dim=-1) * k.norm(dim=-1).max()
+            loose = 2 * delta[:, None] + (n + 16) * 2.0 ** -24
+            assert ((out[b, h].double() - p @ v).abs() <= (p @ v.abs()) * (loose + (n + 16) * 2.0 ** -24)).all(), (b, h, n)
+            w = before["weights"][b, h, :n + 1].double()
+            w[n] = 0.0
+            w += p.sum(0)
+            tol = (p * loose).sum(0) + (G + 1) * 2.0 ** -24 * w
+            assert ((c.weights[b, h, :n + 1].double() - w).abs() <= tol).all(), (b, h, n)
+            assert torch.equal(c.weights[b, h, n + 1:], before["weights"][b, h, n + 1:])
+    for x in ("kc", "vc", "n", "tok"):
+        assert torch.equal(getattr(c, x), want[x]), x
+
+
+@pytest.mark.parametrize("dtype", [W.WKV_BF16, W.WKV_F16])
+@pytest.mark.parametrize("B,Hq,H,d,cap,layout", [(64, 16, 4, 128, 300, "bhtd"), (7, 32, 32, 128, 700, "bthd"), (52, 64, 8, 64, 200, "bhtd"), (56, 24, 8, 128, 130, "bthd"),
+                                                 (60, 20, 4, 64, 4032, "bhtd"), (56, 16, 4, 128, 5056, "bhtd"), (128, 14, 2, 64, 17, "bthd"), (7, 64, 32, 64, 10112, "bhtd")])
+def test_a_workgroup_a_cache(device, dtype, B, Hq, H, d, cap, layout):
+    g = torch.Generator().manual_seed(cap)
+    counts = torch.randint(0, cap, (B, H), generator=g)
+    counts.view(-1)[:9] = torch.tensor([0, 1, 15, 16, cap - 1, cap, -1, cap + 5, 2 ** 31 - 1])
+    c = Caches(device, counts.tolist(), Hq, H, d, dtype, cap, layout=layout)
+    check_whole(c)
+    check_whole(c, with_tok=False)
+
+
+def test_a_workgroup_a_cache_with_kept_counts_and_infinite_logits(device):
+    c = Caches(device, [100] * 56, 16, 4, 128, W.WKV_BF16, 128, flags=W.WKV_DECODE_KEEP_COUNT)
+    before = c.weights.clone()
+    c.q.fill_(1.0)
+    c.kc[:28, :, 5:30] = -float("inf")
+    c.kc[28:] = -float("inf")
+    c.step()
+    assert (c.n == 100).all() and not torch.isnan(c.weights).any()
+    assert torch.equal(c.weights[:28, :, 5:30], before[:28, :, 5:30]) and torch.equal(c.weights[28:, :, :100], before[28:, :, :100])
+    assert (c.weights[:28, :, :5] > before[:28, :, :5]).any() and ((c.weights[28:, :, 100] - 4.0).abs() < 1e-5).all()
+    assert torch.equal(c.out[28:].view(28, 4, 4, 128), c.vn[28:, :, None].float().expand(28, 4, 4, 128))
+    c.kn.fill_(-float("inf"))
+    before = c.weights.clone()
+    c.step()
+    assert torch.equal(c.weights[28:, :, :100], before[28:, :, :100]) and (c.weights[28:, :, 100] == 0).all()
+
+
+def test_a_workgroup_a_cache_captured_and_replayed(device):
+    c = Caches(device, [200 + i for i in range(64)], 16, 4, 128, W.WKV_BF16, 300)
+    names = ("kc", "vc", "n", "weights", "tok", "out")
+    c.step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        W.wkv_decode_step_weighted(c.shape, c.q, c.kn, c.vn, c.kc, c.vc, c.n, c.weights, c.tok, c.at, c.out, c.ws)
+    for step in range(3):
+        c.q.copy_(torch.randn_like(c.q.float()))
+        c.at += 1
+        state = [getattr(c, x).clone() for x in names]
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [getattr(c, x).clone() for x in names]
+        for x, y in zip(names, state):
+            getattr(c, x).copy_(y)
+        check_whole(c)
+        for x, y in zip(names, got):
+            assert torch.equal(getattr(c, x), y), x
