@@ -929,12 +929,14 @@ static void launch_partial_g(const DecodeShape &s, dim3 grid, const void *q, con
 #undef WKV_PARTIAL
 }
 
-// Whether one workgroup takes all rows of a (sequence, KV head), and the launch that does: where they fill the compute units, one or two to each, and
-// the logits of full caches fit into half a unit's LDS.  The logits make no trip through memory then (34 MB written among the rows' reads cost the launch of 64
+// Whether one workgroup takes all rows of a (sequence, KV head), and the launch that does: where these fill the compute units, one or two to each, or
+// their caches are short, and the logits of full caches fit into half a unit's LDS.  The logits make no trip through memory then (34 MB written among the rows' reads cost the launch of 64
 // sequences 20 of 187 us), and there is no second launch; but nobody takes over a long cache's rows.  us by ranges / so, 32q/8kv heads of 128
 // channels, 4128 rows, three sets of caches in turn: 16 sequences 60 / 66, 20 71 / 68, 28 97 / 81, 32 107 / 92, 34 118 / 133, 44 148 / 145, 52 168 / 160,
 // 64 203 / 179, 128 411 / 361; 1000 rows, 32 33.0 / 26.7, 52 48 / 42, 64 59 / 48; mixed, 500 to 4000 rows, 24 57 / 59, 28 68 / 65, 32 83 / 72, 48 92 / 103,
-// 52 113 / 105, 64 133 / 119; one of 4500 rows among 63 of 300 46 / 60; 64 channels, 64q/8kv, 2000 rows, 32 40 / 34, 64 70 / 54.  With 128 channels and more than four
+// 52 113 / 105, 64 133 / 119; one of 4500 rows among 63 of 300 46 / 60; 64 channels, 64q/8kv, 2000 rows, 32 40 / 34, 64 70 / 54.  Nor is there much to take over
+// where every wave's rows are one trip to memory: one sequence of 60 rows 7.9 / 5.1, 250 8.9 / 7.3, 380 8.6 / 9.1, 1000 8.6 / 15.3, twelve of 60 7.8 / 5.2,
+// of 250 9.7 / 7.9, of 380 12.1 / 11.5.  With 128 channels and more than four
 // heads the registers of two workgroups a unit do not suffice.  Values stream, keys do not (both: 64 of 4128 rows 180, mixed ones 127).
 template <int D, int G, bool F16>
 static bool launch_whole(const DecodeShape &s, const void *q, const void *kc, const void *vc, int32_t *n_valid, const DecodeWeights &w, hipStream_t stream) {
@@ -943,7 +945,8 @@ static bool launch_whole(const DecodeShape &s, const void *q, const void *kc, co
   } else {
     constexpr int UNITS = 256;
     const int rows = s.B * s.Hkv;
-    if (!((rows >= UNITS * 7 / 8 && rows <= UNITS) || rows >= UNITS * 13 / 8)) return false;
+    const bool a_round = s.capacity <= WHOLE_THREADS / 64 * 32, fills = (rows >= UNITS * 7 / 8 && rows <= UNITS) || rows >= UNITS * 13 / 8;
+    if (!a_round && !fills) return false;
     if (((int64_t)s.capacity + 15) / 16 * 16 * G > WHOLE_FLOATS) return false;
     hipLaunchKernelGGL((decode_partial_mfma_kernel<D, G, F16, 1, WHOLE_THREADS, true, true>), dim3(rows), dim3(WHOLE_THREADS), 0, stream, s,
                        (const uint16_t *)q, (const uint16_t *)kc, (const uint16_t *)vc, n_valid, (float *)nullptr, w);
