@@ -505,7 +505,7 @@ wkv_status wkv_prefill_attention(const wkv_attention_shape *shape, const void *q
  *   position   device int32 [batch], or NULL with tok_idx: position of the new token
  * A step sets the new row's weight and adds to the others, so each array of weights belongs to one layer: layers that share their row counts have
  * an array each, or one of them decides for all (the others take wkv_decode_step).
- * Everything else as at wkv_decode_step, with a 256-byte-aligned workspace of wkv_decode_weighted_workspace_bytes (contents on entry
+ * Everything else as at wkv_decode_step (sums may be taken in another order), with a 256-byte-aligned workspace of wkv_decode_weighted_workspace_bytes (contents on entry
  * irrelevant; calls that may overlap in time need workspaces of their own) and capacity <= 2^30.  A (b, h) that cannot take the new row leaves its
  * weights and positions as they are, too; where no row of a head weighs anything (all logits -inf), its weights count as 0.
  */

@@ -191,6 +191,10 @@ struct KeyRange {
   }
 };
 
+// What a kernel is given of the weights.  (Nothing where there are none.)
+struct NoWeights {};
+template <bool WEIGHTS> using WeightsOf = std::conditional_t<WEIGHTS, DecodeWeights, NoWeights>;
+
 // WEIGHTS, here and below: the step that accumulates attention weights.  The logits and the row counts are kept for its merge launch, whose
 // workgroups add up the weights (a row's normaliser is not known before).  4 bytes a row and head, written and read, beside 2 * D elements.
 template <typename T, int D, int G, bool STREAM, bool WEIGHTS>
@@ -198,7 +202,7 @@ __global__ __launch_bounds__(DEC_THREADS) void decode_partial_kernel(DecodeShape
                                                                      const T *__restrict__ k_cache,
                                                                      const T *__restrict__ v_cache,
                                                                      const int32_t *__restrict__ n_valid,
-                                                                     float *__restrict__ part, DecodeWeights w) {
+                                                                     float *__restrict__ part, WeightsOf<WEIGHTS> w) {
   constexpr int E = Piece<T>::E;
   constexpr int LPK = D / E;                 // lanes per row
   constexpr int KPT = 64 / LPK;              // rows per wave load instruction
@@ -209,7 +213,8 @@ __global__ __launch_bounds__(DEC_THREADS) void decode_partial_kernel(DecodeShape
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int slot = lane / LPK, piece = lane % LPK;
   const int n = item.n, c0 = split * s.chunk, cend = min(c0 + s.chunk, n < s.capacity ? n : 0);
-  if (WEIGHTS && split == 0 && threadIdx.x == 0) w.counts[bh] = n;
+  if constexpr (WEIGHTS)
+    if (split == 0 && threadIdx.x == 0) w.counts[bh] = n;
   if (nothing_to_do<G>(s, bh, split, n, c0, cend, part)) return;
 
   const T *kc = k_cache + (int64_t)b * s.sb + (int64_t)h * s.sh;
@@ -264,7 +269,8 @@ __global__ __launch_bounds__(DEC_THREADS) void decode_partial_kernel(DecodeShape
         for (int c = 0; c < E; ++c) a = fmaf(qv[g][c], kf[c], a);
         a = row_lanes_sum<LPK>(a);
         sc[u][g] = j < cend ? a : -INFINITY;
-        if (WEIGHTS && piece == g && j < cend) *logit_at(s, w, bh, g, j) = a;
+        if constexpr (WEIGHTS)
+          if (piece == g && j < cend) *logit_at(s, w, bh, g, j) = a;
       }
     }
 #pragma unroll
@@ -436,7 +442,7 @@ __device__ __forceinline__ void finish_whole(const DecodeShape &s, const DecodeW
 template <int D, int G, bool F16, int STREAM, int NT, bool WEIGHTS, bool WHOLE = false>
 __global__ __launch_bounds__(NT, WHOLE ? 4 : 3) void decode_partial_mfma_kernel(
     DecodeShape s, const uint16_t *__restrict__ q_new, const uint16_t *k_cache,
-    const uint16_t *v_cache, const int32_t *__restrict__ n_valid, float *__restrict__ part, DecodeWeights w) {
+    const uint16_t *v_cache, const int32_t *__restrict__ n_valid, float *__restrict__ part, WeightsOf<WEIGHTS> w) {
   constexpr int E = 8, WAVES = NT / 64;
   constexpr bool PAIRS = WHOLE || WAVES == DEC_WAVES;
   constexpr int LPK = D / E;                 // lanes per row (value side): 16 or 8
@@ -470,7 +476,8 @@ __global__ __launch_bounds__(NT, WHOLE ? 4 : 3) void decode_partial_mfma_kernel(
       return;
     }
   } else {
-    if (WEIGHTS && split == 0 && threadIdx.x == 0) w.counts[bh] = n;
+    if constexpr (WEIGHTS)
+      if (split == 0 && threadIdx.x == 0) w.counts[bh] = n;
     if (nothing_to_do<G>(s, bh, split, n, c0, cend, part)) return;
   }
 
@@ -526,7 +533,7 @@ __global__ __launch_bounds__(NT, WHOLE ? 4 : 3) void decode_partial_mfma_kernel(
     asm volatile("" : "+v"(first));
     for (int i = first; i < n_kept * (G * 4); i += 64) {
       const int blk = last_blk - (n_kept - 1 - i / (G * 4)) * WAVES;
-      __builtin_nontemporal_store(*(const f32x4 *)&logit_s[wave][i / (G * 4)][i % (G * 4) * 4], (f32x4 *)(logit_at(s, w, bh, 0, c0 + blk * 16) + i % (G * 4) * 4));
+      if constexpr (WEIGHTS) __builtin_nontemporal_store(*(const f32x4 *)&logit_s[wave][i / (G * 4)][i % (G * 4) * 4], (f32x4 *)(logit_at(s, w, bh, 0, c0 + blk * 16) + i % (G * 4) * 4));
     }
     n_kept = 0;
   };
@@ -748,7 +755,7 @@ template <typename T, int D, int NT, bool WEIGHTS>
 __global__ __launch_bounds__(NT) void decode_combine_kernel(DecodeShape s, const T *__restrict__ q_new,
                                                                      const T *__restrict__ k_new, const T *__restrict__ v_new,
                                                                      T *k_cache, T *v_cache, const float *__restrict__ part,
-                                                                     int32_t *n_valid, float *__restrict__ out, DecodeWeights dw) {
+                                                                     int32_t *n_valid, float *__restrict__ out, WeightsOf<WEIGHTS> dw) {
   constexpr int COLS = D / 4, GROUPS = NT / COLS, AHEAD = NT == 64 ? 4 : 6, WAVES = NT / 64;
   constexpr int E = Piece<T>::E, LPK = D / E;
   constexpr bool FEW = NT == 64;
@@ -884,7 +891,7 @@ __global__ __launch_bounds__(NT) void decode_combine_kernel(DecodeShape s, const
 
 template <typename T, int D, int G, bool WEIGHTS>
 static void launch_partial_g(const DecodeShape &s, dim3 grid, const void *q, const void *kc, const void *vc,
-                             const int32_t *n_valid, float *part, const DecodeWeights &w, hipStream_t stream) {
+                             const int32_t *n_valid, float *part, const WeightsOf<WEIGHTS> &w, hipStream_t stream) {
   // Where a model's caches exceed the memory-side cache, no row is found there at the next token, and the values, as both
   // caches in fp32, are best streamed.  How many layers there are and (n_valid is on the device) how many rows the library
   // cannot know: the line is that of 32 layers of full caches.  Us a layer with plain loads / with values streamed, where the rows
@@ -956,7 +963,7 @@ static bool launch_whole(const DecodeShape &s, const void *q, const void *kc, co
 
 template <typename T, int D, bool WEIGHTS>
 static hipError_t launch_decode_t(const DecodeShape &s, const void *q, const void *kn, const void *vn, void *kc, void *vc,
-                                  int32_t *n_valid, float *out, float *part, const DecodeWeights &w, hipStream_t stream) {
+                                  int32_t *n_valid, float *out, float *part, const WeightsOf<WEIGHTS> &w, hipStream_t stream) {
   const dim3 grid(s.B * s.Hkv, s.n_splits);
   if constexpr (WEIGHTS && sizeof(T) == 2) {
     DecodeWeights all = w;
@@ -993,7 +1000,7 @@ static hipError_t launch_decode_t(const DecodeShape &s, const void *q, const voi
 
 template <bool WEIGHTS>
 static hipError_t launch_decode_as(const DecodeShape &s, const void *q_new, const void *k_new, const void *v_new, void *k_cache,
-                                   void *v_cache, int32_t *n_valid, float *out, float *part, const DecodeWeights &w, hipStream_t stream) {
+                                   void *v_cache, int32_t *n_valid, float *out, float *part, const WeightsOf<WEIGHTS> &w, hipStream_t stream) {
 #define WKV_DEC_TYPE(TT) \
   return s.d == 128 ? launch_decode_t<TT, 128, WEIGHTS>(s, q_new, k_new, v_new, k_cache, v_cache, n_valid, out, part, w, stream) \
                     : launch_decode_t<TT, 64, WEIGHTS>(s, q_new, k_new, v_new, k_cache, v_cache, n_valid, out, part, w, stream);
@@ -1011,7 +1018,7 @@ hipError_t launch_decode_weighted(const DecodeShape &s, const void *q_new, const
 #else
 hipError_t launch_decode(const DecodeShape &s, const void *q_new, const void *k_new, const void *v_new, void *k_cache,
                          void *v_cache, int32_t *n_valid, float *out, float *part, hipStream_t stream) {
-  return launch_decode_as<false>(s, q_new, k_new, v_new, k_cache, v_cache, n_valid, out, part, DecodeWeights(), stream);
+  return launch_decode_as<false>(s, q_new, k_new, v_new, k_cache, v_cache, n_valid, out, part, NoWeights(), stream);
 }
 
 constexpr int MAX_DEVICES = 64;
