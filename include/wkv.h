@@ -489,7 +489,8 @@ size_t wkv_attention_workspace_bytes(const wkv_attention_shape *shape);
  *              q_len[b] - lse_rows + r, -inf where there is no such row.  With lse_rows = w_obs it is the lse_obs
  *              that wkv_score and wkv_compress_groups take.
  * Logits, softmax and output sums are fp32; 16-bit types round a probability (relative to the row's reference) to their own type for the
- * product with the values, and the output once.  Results do not change from run to run.
+ * product with the values (by half a step; in fp16 by 2^-38 of the row's sum where that is more), and the output once.  Results do not change from
+ * run to run.
  */
 wkv_status wkv_prefill_attention(const wkv_attention_shape *shape, const void *q, const void *k, const void *v, void *out,
                                  float *lse_out, void *workspace, size_t workspace_bytes, void *hip_stream);
