@@ -38,7 +38,6 @@ static __device__ __align__(256) unsigned char scratch[WKV_DECODE_STATIC_SCRATCH
 
 constexpr int DEC_THREADS = 256;
 constexpr int DEC_WAVES = DEC_THREADS / 64;
-constexpr int WHOLE_THREADS = 512, WHOLE_FLOATS = 20224;      // logits in LDS: two workgroups a compute unit, 80 KB each
 constexpr int WIDE_THREADS = 512;   // where a range is a block for each of eight waves (see launch_partial_g)
 constexpr int DEC_U = 4;            // row tiles per wave batch (loads in flight: 2 * DEC_U per lane)
 
@@ -525,7 +524,7 @@ __global__ __launch_bounds__(NT, WHOLE ? 4 : 3) void decode_partial_mfma_kernel(
   };
   // WEIGHTS: a wave collects its logits in LDS, ROUND blocks at a time.  Stored as they come, they would be waited for with every round's rows (stores and
   // loads are counted together), and in registers they cost a wave a SIMD: 64 sequences of 4128 rows 246 and 232 us a step, 203 so.  (Plain stores
-  // leave 34 MB to be written back behind the launch, 217; without any 178: launch_whole.)
+  // leave 34 MB to be written back behind the launch, 217; without any 178: decode_takes_whole_caches.)
   int n_kept = 0;
   auto store_logits = [&](int last_blk) __attribute__((always_inline)) {        // those of the last n_kept blocks, up to last_blk
     __builtin_amdgcn_wave_barrier();
@@ -936,28 +935,15 @@ static void launch_partial_g(const DecodeShape &s, dim3 grid, const void *q, con
 #undef WKV_PARTIAL
 }
 
-// Whether one workgroup takes all rows of a (sequence, KV head), and the launch that does: where these fill the compute units, one or two to each, or
-// their caches are short, and the logits of full caches fit into half a unit's LDS.  The logits make no trip through memory then (34 MB written among the rows' reads cost the launch of 64
-// sequences 20 of 187 us), and there is no second launch; but nobody takes over a long cache's rows.  us by ranges / so, 32q/8kv heads of 128
-// channels, 4128 rows, three sets of caches in turn: 16 sequences 60 / 66, 20 71 / 68, 28 97 / 81, 32 107 / 92, 34 118 / 133, 44 148 / 145, 52 168 / 160,
-// 64 203 / 179, 128 411 / 361; 1000 rows, 32 33.0 / 26.7, 52 48 / 42, 64 59 / 48; mixed, 500 to 4000 rows, 24 57 / 59, 28 68 / 65, 32 83 / 72, 48 92 / 103,
-// 52 113 / 105, 64 133 / 119; one of 4500 rows among 63 of 300 46 / 60; 64 channels, 64q/8kv, 2000 rows, 32 40 / 34, 64 70 / 54.  Nor is there much to take over
-// where every wave's rows are one trip to memory: one sequence of 60 rows 7.9 / 5.1, 250 8.9 / 7.3, 380 8.6 / 9.1, 1000 8.6 / 15.3, twelve of 60 7.8 / 5.2,
-// of 250 9.7 / 7.9, of 380 12.1 / 11.5.  With 128 channels and more than four
-// heads the registers of two workgroups a unit do not suffice.  Values stream, keys do not (both: 64 of 4128 rows 180, mixed ones 127).
+// A workgroup a cache (decode_takes_whole_caches has both sides of the choice).  Values stream, keys do not (both: 64 sequences of 4128 rows 180 us, mixed ones 127).
 template <int D, int G, bool F16>
-static bool launch_whole(const DecodeShape &s, const void *q, const void *kc, const void *vc, int32_t *n_valid, const DecodeWeights &w, hipStream_t stream) {
-  if constexpr (D == 128 && G > 4) {
-    return false;
+static hipError_t launch_whole(const DecodeShape &s, const void *q, const void *kc, const void *vc, int32_t *n_valid, const DecodeWeights &w, hipStream_t stream) {
+  if constexpr (D == 128 && G > 4) {         // (never chosen)
+    return hipErrorInvalidValue;
   } else {
-    constexpr int UNITS = 256;
-    const int rows = s.B * s.Hkv;
-    const bool a_round = s.capacity <= WHOLE_THREADS / 64 * 32, fills = (rows >= UNITS * 7 / 8 && rows <= UNITS) || rows >= UNITS * 13 / 8;
-    if (!a_round && !fills) return false;
-    if (((int64_t)s.capacity + 15) / 16 * 16 * G > WHOLE_FLOATS) return false;
-    hipLaunchKernelGGL((decode_partial_mfma_kernel<D, G, F16, 1, WHOLE_THREADS, true, true>), dim3(rows), dim3(WHOLE_THREADS), 0, stream, s,
+    hipLaunchKernelGGL((decode_partial_mfma_kernel<D, G, F16, 1, WHOLE_THREADS, true, true>), dim3(s.B * s.Hkv), dim3(WHOLE_THREADS), 0, stream, s,
                        (const uint16_t *)q, (const uint16_t *)kc, (const uint16_t *)vc, n_valid, (float *)nullptr, w);
-    return true;
+    return hipGetLastError();
   }
 }
 
@@ -965,16 +951,17 @@ template <typename T, int D, bool WEIGHTS>
 static hipError_t launch_decode_t(const DecodeShape &s, const void *q, const void *kn, const void *vn, void *kc, void *vc,
                                   int32_t *n_valid, float *out, float *part, const WeightsOf<WEIGHTS> &w, hipStream_t stream) {
   const dim3 grid(s.B * s.Hkv, s.n_splits);
-  if constexpr (WEIGHTS && sizeof(T) == 2) {
-    DecodeWeights all = w;
-    all.k_new = kn; all.v_new = vn; all.n_valid = n_valid; all.out = out;
-#define WKV_WHOLE(GG) case GG: if (launch_whole<D, GG, !__is_same(T, uint16_t)>(s, q, kc, vc, n_valid, all, stream)) return hipGetLastError(); break;
-    switch (s.G) {
-      WKV_WHOLE(1) WKV_WHOLE(2) WKV_WHOLE(3) WKV_WHOLE(4) WKV_WHOLE(5) WKV_WHOLE(6) WKV_WHOLE(7) WKV_WHOLE(8)
-      default: break;
-    }
+  if constexpr (WEIGHTS && sizeof(T) == 2)
+    if (decode_takes_whole_caches(s)) {
+      DecodeWeights all = w;
+      all.k_new = kn; all.v_new = vn; all.n_valid = n_valid; all.out = out;
+#define WKV_WHOLE(GG) case GG: return launch_whole<D, GG, !__is_same(T, uint16_t)>(s, q, kc, vc, n_valid, all, stream);
+      switch (s.G) {
+        WKV_WHOLE(1) WKV_WHOLE(2) WKV_WHOLE(3) WKV_WHOLE(4) WKV_WHOLE(5) WKV_WHOLE(6) WKV_WHOLE(7) WKV_WHOLE(8)
+        default: return hipErrorInvalidValue;
+      }
 #undef WKV_WHOLE
-  }
+    }
 #define WKV_DEC_CASE(GG) \
   case GG: launch_partial_g<T, D, GG, WEIGHTS>(s, grid, q, kc, vc, n_valid, part, w, stream); break;
   switch (s.G) {

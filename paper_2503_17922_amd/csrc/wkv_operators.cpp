@@ -229,6 +229,27 @@ size_t decode_weighted_layout(const DecodeShape &s, size_t partial_bytes, size_t
   return *logits_at + rows * s.G * s.n_splits * s.chunk * sizeof(float);
 }
 
+// Where the pairs of sequence and KV head fill the compute units, one or two to each, or their caches are short, and the logits of full caches fit into half a unit's LDS.  The
+// logits make no trip through memory then (34 MB written among the rows' reads cost the launch of 64 sequences 20 of 187 us), and there is no second
+// launch; but nobody takes over a long cache's rows.  us by ranges / so, 32q/8kv heads of 128 channels, 4128 rows, three sets of caches in turn: 16 sequences 60 / 66, 20 71 / 68, 28
+// 97 / 81, 32 107 / 92, 34 118 / 133, 44 148 / 145, 52 168 / 160, 64 203 / 179, 128 411 / 361; 4383 rows, 65 243 / 232, 72 254 / 241, 88 309 / 260, 144 518 / 440; 1000 rows, 32
+// 33.0 / 26.7, 52 48 / 42, 64 59 / 48, 65 60 / 58, 129 114 / 101; mixed, 500 to 4000 rows, 24 57 / 59, 28 68 / 65, 32 83 / 72, 48 92 / 103, 52 113 / 105, 64 133 / 119; 64 channels,
+// 64q/8kv, 2000 rows, 32 40 / 34, 64 70 / 54.
+// How many rows a cache has is on the device, and a single long one among short ones loses by this: all caches full, mixed (an eighth on), one full among caches of 8
+// rows: 32 sequences of 5055 rows 131 / 111, 86 / 81, 25 / 58, 64 of them 253 / 220, 183 / 157, 37 / 58; 16q/8kv, 10111 rows, 32 241 / 214, 156 / 153, 45 / 105, 64
+// 479 / 428, 331 / 302, 58 / 105.  Past that, where 128 channels of one query head alone could go, there is little to gain: 8q/8kv, 20223 rows, 32 460 / 431, 284 / 299, 85 / 202, 64
+// 919 / 857, 619 / 598, 108 / 203; 64 channels, 64 of them 555 / 458, 402 / 327, 78 / 108.
+// Nor is there much to take over where every wave's rows are one trip to memory: one sequence of 60 rows 7.9 / 5.1, 250 8.9 / 7.3, 380 8.6 / 9.1, 1000
+// 8.6 / 15.3, twelve of 60 7.8 / 5.2, of 250 9.7 / 7.9, of 380 12.1 / 11.5.  With 128 channels and more than four heads the registers of two
+// workgroups a unit do not suffice.
+bool decode_takes_whole_caches(const DecodeShape &s) {
+  constexpr int32_t UNITS = 256;
+  if (s.dtype == WKV_F32 || (s.d == 128 && s.G > 4)) return false;
+  const int32_t rows = s.B * s.Hkv;
+  const bool a_round = s.capacity <= WHOLE_THREADS / 64 * 32, fills = (rows >= UNITS * 7 / 8 && rows <= UNITS) || rows >= UNITS * 13 / 8;
+  return (a_round || fills) && ceil_div(s.capacity, 16) * 16 * std::max(s.G, s.d / 64) <= WHOLE_FLOATS;
+}
+
 size_t evict_layout(int32_t rows, int32_t max_moves, size_t *moves_at) {
   *moves_at = round_up((size_t)rows * sizeof(int32_t));
   return *moves_at + (size_t)rows * max_moves * sizeof(int2);

@@ -58,6 +58,10 @@ hipError_t launch_attention(const AttentionPlan &plan, const void *q, const void
                             hipStream_t stream);
 
 // ---- decode step with weights ---------------------------------------------------------------------
+// Whether one workgroup takes all rows of a (sequence, KV head), whose logits stay in its LDS, instead of ranges of them: with two workgroups to a compute unit,
+// 80 KB each.
+constexpr int32_t WHOLE_THREADS = 512, WHOLE_FLOATS = 20224;
+bool decode_takes_whole_caches(const DecodeShape &s);
 // Behind the partial results in the workspace: the row counts of this step, int32 [B*Hkv], then the logits (base 2),
 // float [B*Hkv][n_splits * chunk / 16][G][16].
 struct DecodeWeights {
