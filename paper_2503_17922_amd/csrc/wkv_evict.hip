@@ -337,12 +337,15 @@ hipError_t launch_evict(const EvictArgs &a, const EvictLayers &layers, int32_t n
 #undef WKV_SELECT
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  // Workgroups for as many moves as there can be, one round of a thread's each: how many there are is on the device, and a workgroup without any
-  // costs little (eight sequences, 4 layers, 236 MB to move: 66.0 us; with a quarter of them, four rounds each, 69.2; moves two at a time
-  // 66.5).  Nontemporal: plain stores leave their write-back to the next kernel (71.6).
+  // Workgroups for as many moves as there can be, one round of a thread's each: how many there are is on the device (eight sequences, 4 layers, 236 MB to move:
+  // 66.0 us; with a quarter of them, four rounds each, 69.2; moves two at a time 66.5).  But not many more than the chip starts in some 6 us, since most calls of a serving
+  // loop find little or nothing to move.  At most 65536 / 20480 / 8192 of them, us: nothing to drop, 64 sequences of 8 heads, 4 layers 18.9 / 11.9 / 6.8, 32 layers 31 / 17 / 17, 32
+  // sequences 11.1 / 10.3 / 6.6; one row too many in each of 64 51.5 / 33 / 28.5; sixteen cut from 8192 rows to 4096 211 / 216 / 224; the eight sequences 63.8 / 63.8 / 66.
+  // (16384, rows of all workgroups a power of two apart: 65; a workgroup's moves side by side instead of one of each stretch 70 to 102.)
+  // Nontemporal: plain stores leave their write-back to the next kernel (71.6).
   const int lpr = a.row_bytes / 16, rows_at_once = MOVE_THREADS / lpr;
   const int64_t most = (a.max_moves + MOVE_AHEAD * rows_at_once - 1) / (MOVE_AHEAD * rows_at_once), pairs = (int64_t)a.rows * n_layers * 2;
-  const int64_t want = std::min(most, std::max<int64_t>(65536 / pairs, 1));
+  const int64_t want = std::min(most, std::max<int64_t>(20480 / pairs, 1));
   const dim3 grid((uint32_t)want, a.rows, n_layers * 2);
 #define WKV_MOVE(LPR) hipLaunchKernelGGL((evict_move_kernel<LPR>), grid, dim3(MOVE_THREADS), 0, stream, a, layers, counts, moves)
   if (lpr == 8) WKV_MOVE(8);
