@@ -478,8 +478,9 @@ typedef struct {
   int64_t out_stride_b, out_stride_h, out_stride_t;
 } wkv_attention_shape;
 
-/* Bytes of 256-byte-aligned device workspace wkv_prefill_attention needs for exactly these lengths (shorter ones can need more); 0 for an
- * invalid shape.  Its contents on entry are irrelevant and on return unspecified; calls that may overlap in time need workspaces of their own. */
+/* Bytes of 256-byte-aligned device workspace wkv_prefill_attention needs for exactly these lengths (shorter ones can need more, none more than
+ * 2^20 * (4 * head_dim + 8) + 512, 545 MB with 128 channels); 0 for an invalid shape.  Its contents on entry are irrelevant and on return
+ * unspecified; calls that may overlap in time need workspaces of their own. */
 size_t wkv_attention_workspace_bytes(const wkv_attention_shape *shape);
 
 /*

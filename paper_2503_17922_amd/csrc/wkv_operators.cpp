@@ -201,8 +201,13 @@ wkv_status plan_attention(const wkv_attention_shape *p, AttentionPlan *plan) {
   // (a sequence without rows has a block for the normalisers of rows that do not exist)
   for (int32_t b = 0; b < p->batch; ++b)
     a.seq[b].blocks = (int32_t)std::max<int64_t>(ceil_div((int64_t)a.seq[b].q_len * a.G, plan->rows), p->lse_rows > 0 ? 1 : 0);
-  std::sort(a.seq, a.seq + p->batch, [](const AttentionSeq &x, const AttentionSeq &y) { return x.blocks != y.blocks ? x.blocks > y.blocks : x.b < y.b; });
-  int64_t items = 0;
+  // (and goes last: its block leaves no partial results and has no room for any)
+  std::sort(a.seq, a.seq + p->batch, [](const AttentionSeq &x, const AttentionSeq &y) {
+    if (x.blocks != y.blocks) return x.blocks > y.blocks;
+    return (x.q_len == 0) != (y.q_len == 0) ? y.q_len == 0 : x.b < y.b;
+  });
+  int64_t items = 0, idle = 0;
+  for (int32_t b = 0; b < p->batch; ++b) idle += a.seq[b].q_len == 0 ? (int64_t)a.seq[b].blocks * a.Hkv : 0;
   for (int32_t i = 0; i < WKV_MAX_BATCH; ++i) {
     if (i < p->batch) items += (int64_t)(a.seq[i].blocks - (i + 1 < p->batch ? a.seq[i + 1].blocks : 0)) * (i + 1) * a.Hkv;
     if (items > 1 << 23) { set_error("more than 2^23 blocks of %d rows; split the call", plan->rows); return WKV_ERR_UNSUPPORTED; }      // (launch grid limit)
@@ -215,7 +220,7 @@ wkv_status plan_attention(const wkv_attention_shape *p, AttentionPlan *plan) {
   a.fold_parts = items % 8 == 0 ? 0 : 0x7fffffff;
   plan->ws_bytes = 256;
   if (a.splits > 1) {
-    const size_t rows = (size_t)items * a.splits * plan->rows;
+    const size_t rows = (size_t)(items - idle) * a.splits * plan->rows;        // at most 2^20: 4096 workgroups of 256 rows (cut_attention)
     plan->stats_at = rows * a.d * sizeof(float);
     plan->ws_bytes = round_up(plan->stats_at + rows * sizeof(float2));
   }

@@ -47,7 +47,7 @@ struct AttentionArgs {
   int32_t fold_from, fold_parts;         // from these workgroups on the items go the other way round (wkv_attention.hip, item_of)
 };
 // Partial results in the workspace, of blocks that more than one workgroup shares: outputs float [items][splits][rows][d], then
-// their references and sums float2 [items][splits][rows].
+// their references and sums float2 [items][splits][rows], both without the last items, those of sequences that have no rows.
 struct AttentionPlan {
   AttentionArgs args;
   int32_t items, rows, most_rows;        // blocks, their rows, and the most that any of them has
