@@ -24,6 +24,7 @@ bool known_dtype(int32_t dtype) {
   set_error("unknown dtype %d", dtype);
   return false;
 }
+constexpr int64_t MAX_STRIDE = (int64_t)1 << 48;      // the address space ends there; products with the bytes of an element and the rows of a tile fit 64 bits
 // Row starts at multiples of 16 bytes, rows of head_dim channels that do not overlap.
 bool good_strides(int32_t dtype, int32_t head_dim, int64_t sb, int64_t sh, int64_t st, const char *what) {
   const int64_t vec = 16 / elem_bytes(dtype);
@@ -31,6 +32,7 @@ bool good_strides(int32_t dtype, int32_t head_dim, int64_t sb, int64_t sh, int64
     set_error("%s strides must be non-negative multiples of %lld elements (16 bytes)", what, (long long)vec);
     return false;
   }
+  if (std::max({sb, sh, st}) > MAX_STRIDE) { set_error("%s strides must be at most 2^48 elements", what); return false; }
   if (st < head_dim || sh < head_dim) { set_error("%s token and head strides must be >= head_dim", what); return false; }
   return true;
 }
@@ -262,7 +264,9 @@ size_t evict_layout(int32_t rows, int32_t max_moves, size_t *moves_at) {
 // (row numbers and the ends of key ranges stay below 2^31)
 static wkv_status validate_cache(const wkv_decode_shape *shape, Decode *dc) {
   const wkv_status st = validate_decode(shape, dc);
-  if (st != WKV_OK || dc->shape.capacity <= 1 << 30) return st;
+  if (st != WKV_OK) return st;
+  if (std::max({dc->shape.sb, dc->shape.sh, dc->shape.st}) > MAX_STRIDE) { set_error("cache strides must be at most 2^48 elements"); return WKV_ERR_INVALID_ARG; }
+  if (dc->shape.capacity <= 1 << 30) return WKV_OK;
   set_error("capacity %d is not supported (at most 2^30 rows)", dc->shape.capacity);
   return WKV_ERR_UNSUPPORTED;
 }
