@@ -486,6 +486,7 @@ size_t wkv_attention_workspace_bytes(const wkv_attention_shape *shape);
 /*
  *   q, k, v    device, layouts above.  Keys and values of the k_len rows must be finite; other rows may hold anything.
  *   out        device, layout above; must not overlap the inputs, nor a row another row
+ *   (q and out may be NULL where no sequence has rows, k and v where none that has rows has keys)
  *   lse_out    device float32 [batch, n_q_heads, lse_rows] (contiguous), or NULL with lse_rows = 0: entry r belongs to row
  *              q_len[b] - lse_rows + r, -inf where there is no such row.  With lse_rows = w_obs it is the lse_obs
  *              that wkv_score and wkv_compress_groups take.

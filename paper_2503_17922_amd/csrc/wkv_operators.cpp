@@ -343,11 +343,17 @@ wkv_status wkv_prefill_attention(const wkv_attention_shape *shape, const void *q
   AttentionPlan plan;
   wkv_status st = plan_attention(shape, &plan);
   if (st != WKV_OK) return st;
-  if (!q || !k || !v || !out) return invalid("q / k / v / out is NULL");
+  // (tensors without elements may have no address)
+  bool rows = false, pairs = false;
+  for (int32_t i = 0; i < plan.args.n_seqs; ++i) {
+    const AttentionSeq &sq = plan.args.seq[i];
+    rows |= sq.q_len > 0; pairs |= sq.q_len > 0 && sq.k_len > 0;
+  }
+  if ((rows && (!q || !out)) || (pairs && (!k || !v))) return invalid("q / k / v / out is NULL");
   if (misaligned(q, 16) || misaligned(k, 16) || misaligned(v, 16) || misaligned(out, 16)) return invalid("q, k, v and out must be 16-byte aligned");
   if (plan.args.lse_rows > 0 && !lse_out) return invalid("lse_out is NULL and lse_rows is not 0");
   if (misaligned(lse_out, 4)) return invalid("lse_out must be 4-byte aligned");
-  if (out == q || out == k || out == v) return invalid("out must not overlap the inputs");
+  if (out && (out == q || out == k || out == v)) return invalid("out must not overlap the inputs");
   st = check_workspace(workspace, workspace_bytes, plan.ws_bytes);
   if (st != WKV_OK) return st;
   if (plan.items == 0) return WKV_OK;
