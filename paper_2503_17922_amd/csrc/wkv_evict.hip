@@ -205,7 +205,8 @@ __device__ __forceinline__ int evict_rows(const EvictArgs &a, EvictLds &lds, uin
   return (int)all;
 }
 
-// Any number of rows: the same steps, with the weights read in each.
+// Any number of rows: the same steps, with the weights read in each, and the first digit over all keys.  (What fits LDS goes the way above: eight sequences of 8 heads,
+// 2 layers, a tenth of 16384 rows dropped 64 us the call, of 32768 222, so; two of 131072 456.)
 __device__ __forceinline__ int evict_long(const EvictArgs &a, EvictLds &lds, int n, int stay, float *w, int32_t *tok, int2 *mv) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Range r(n, wave);
