@@ -8,8 +8,8 @@
 //                  which a lane holds them; the values are read to match (16 bits: transposed, ds_read_tr; four keys of a channel)
 // The rows of a block are (query, head of the group) pairs, query-major: the G heads that share a KV head share its tiles.
 //
-// Long prompts are bound by the matrix pipe at the clock that power leaves it: 32768 tokens of 32q/8kv heads with 128 channels in bf16 take 7.6 to 8.0 ms from chip to chip =
-// 1100-1150 TFLOP/s (a library product of 8192^3 1202-1275; the same call on zeros 5.8 ms): by the counters 56 % of the matrix cycles at 1.9 GHz.  Short ones are bound by a
+// Long prompts are bound by the matrix pipe at the clock that power leaves it: 32768 tokens of 32q/8kv heads with 128 channels in bf16 take 7.4 to 8.0 ms from chip to chip =
+// 1100-1190 TFLOP/s (a library product of 8192^3 1202-1275; the same call on zeros 5.8 ms): by the counters 56 % of the matrix cycles at 1.9 to 2.0 GHz.  Short ones are bound by a
 // wave's chain of products, statistics and products, 1.2 us a tile.  Eight waves of 32 rows, all at the same tile, fetch it once: 7.67 ms, by workgroups of four
 // 7.84 (4096 tokens 133 and 146 us).  No better: 64 rows a wave with a SIMD for itself, so that a fragment from LDS feeds two products (9.07; with the next tile's
 // logits computed beside this one's exponentials the registers do not suffice); a reference that moves when a tile's sum overflows, without

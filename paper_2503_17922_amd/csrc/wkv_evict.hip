@@ -7,7 +7,7 @@
 //                   place, and one row too many costs one row's copy instead of half a cache's.
 //   move kernel     copies the rows of every layer's keys and values.
 // The selection reads 8 bytes a row and is a chain of scans, bound by their latency (4097 rows: 20.6 us with the weights read anew in every
-// step and fixed digits, 9.9 so); the copies by memory, in pieces of a row here and there (5 TB/s).
+// step and fixed digits, 9 to 10 so); the copies by memory, in pieces of a row here and there (5 TB/s).
 #include <algorithm>
 
 #include "wkv_device.h"
