@@ -539,6 +539,168 @@ wkv_status wkv_cache_evict(const wkv_decode_shape *shape, int32_t n_layers, void
                            float *weights, int32_t *tok_idx, int32_t *n_valid, const int32_t *keep, int32_t recent,
                            void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/*
+ * ---- generation: norms with rotary positions, caches in 8 and 4 bits, trees of drafted tokens --------------------
+ *
+ * Queries and keys normalised a head at a time and turned by their positions in one pass.  With a weight w (the queries' or the
+ * keys'; NULL: those heads are not normalised), every head's row x of head_dim channels becomes
+ *     y = x * w / sqrt(mean(x^2) + eps)
+ * and the pairs of y's first rotary_dim channels are turned as by wkv_rope, pair i by the angle positions[axis_of_pair[i]] * inv_freq[i]:
+ * text has one axis, images and videos one for each of time, height, width.  Computed in fp32 (the angle is reduced exactly), rounded once.
+ */
+#define WKV_ROPE_MAX_AXES 4
+typedef struct {
+  int32_t batch;             /* >= 1                                                      */
+  int32_t n_tokens;          /* >= 0: rows per sequence; batch * n_tokens <= 2^25       */
+  int32_t n_q_heads;         /* >= 0; 0: no queries (q_in, q_out, q_weight are not read)   */
+  int32_t n_kv_heads;        /* >= 0; 0: no keys                                          */
+  int32_t head_dim;          /* 64 or 128                                                 */
+  int32_t rotary_dim;        /* multiple of 16, 16 .. head_dim                            */
+  int32_t dtype;             /* wkv_dtype of the four tensors and of the weights          */
+  int32_t flags;             /* 0 or WKV_ROPE_INTERLEAVED                                 */
+  int32_t n_axes;            /* 1 .. WKV_ROPE_MAX_AXES                                    */
+  float   eps;               /* finite, >= 0                                              */
+  double  amplitude;         /* factor of the rotated channels; 0 selects 1               */
+  const double *inv_freq;    /* host [rotary_dim / 2], finite; see wkv_rope_frequencies   */
+  const int32_t *axis_of_pair;       /* host [rotary_dim / 2], 0 .. n_axes - 1, or NULL: axis 0 for all     */
+  int64_t q_stride_b, q_stride_h, q_stride_t;                /* q_in  [batch, n_q_heads, n_tokens, head_dim], elements */
+  int64_t q_out_stride_b, q_out_stride_h, q_out_stride_t;    /* q_out                      */
+  int64_t k_stride_b, k_stride_h, k_stride_t;                /* k_in  [batch, n_kv_heads, n_tokens, head_dim]          */
+  int64_t k_out_stride_b, k_out_stride_h, k_out_stride_t;    /* k_out, e.g. rows of a cache                            */
+} wkv_norm_rope_shape;
+
+/*
+ *   positions     device int32 [batch, n_tokens, n_axes], contiguous; a row with a negative position on any axis (padding) is left as it is
+ *   q_weight,
+ *   k_weight      device [head_dim], 16-byte aligned, or NULL
+ *   q_in ...      as at wkv_rope: 16-byte aligned, strides multiples of 16 bytes, in place with the same strides or without overlap
+ * Without weights and with one axis the results are those of wkv_rope up to the order of their roundings.  The squares of a normalised row must sum to less
+ * than fp32's largest number.  A row of zeros with eps = 0 gives NaN.  No workspace; calls on
+ * different streams may overlap in time.
+ */
+wkv_status wkv_norm_rope(const wkv_norm_rope_shape *shape, const int32_t *positions, const void *q_weight, const void *k_weight,
+                         const void *q_in, void *q_out, const void *k_in, void *k_out, void *hip_stream);
+
+/*
+ * Caches in 8 and 4 bits.  Every 32 channels of a row share a scale, a power of two 2^(s - 127) held as the byte s; a row is
+ *   codes   WKV_CACHE_E4M3: head_dim bytes, 8-bit floats (4 exponent bits biased by 7, 3 fraction bits, magnitudes up to 448)
+ *           WKV_CACHE_E2M1: head_dim / 2 bytes, 4-bit floats (2 exponent bits biased by 1, 1 fraction bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a
+ *           sign), the even channel of a byte in its lower half
+ *   scales  head_dim / 32 bytes
+ * and a channel stands for code * scale.  A group's scale is the smallest power of two, at least 2^-100, with which none of its magnitudes exceeds the format's
+ * largest code, so that nothing is cut off; a channel gets the nearest code, of two equally near ones the even one.  Zeros give s = 27 and
+ * codes 0.  A group that holds an infinity, a NaN or a magnitude above 2^127 stands for NaN in all its channels (s = 255, codes 0).
+ *
+ * Tensors: codes uint8 [batch, n_kv_heads, capacity, bytes of a row] by the strides below; scales uint8
+ * [batch, n_kv_heads, capacity, head_dim / 32], contiguous, 4-byte aligned; of keys and of values.
+ */
+typedef enum { WKV_CACHE_E4M3 = 0, WKV_CACHE_E2M1 = 1 } wkv_cache_format;
+
+typedef struct {
+  int32_t batch;             /* >= 1; batch * n_kv_heads <= 65535                               */
+  int32_t n_q_heads;         /* wkv_decode_step_quantized: multiple of n_kv_heads, at most 8 query heads per KV head; else not used but valid */
+  int32_t n_kv_heads;
+  int32_t head_dim;          /* 64 or 128                                                       */
+  int32_t dtype;             /* wkv_dtype of plain rows, queries and new rows                   */
+  int32_t format;            /* wkv_cache_format                                                */
+  float   scale;             /* logit scale of the decode step; 0 selects 1/sqrt(head_dim)      */
+  int32_t capacity;          /* rows per (b, h) in the caches, at most 2^30                      */
+  int64_t code_stride_b, code_stride_h, code_stride_t;      /* codes: BYTES, multiples of 16; a row contiguous */
+  int32_t flags;             /* 0, or WKV_DECODE_KEEP_COUNT (decode step)                       */
+  int32_t n_rows;            /* wkv_cache_quantize, wkv_cache_dequantize: rows per (b, h) at most, >= 0; batch * n_kv_heads * n_rows <= 2^30  */
+  int32_t row_capacity;      /* wkv_cache_quantize: rows per (b, h) that the plain tensors hold, which tok_idx counts in; >= n_rows without it */
+  int64_t row_stride_b, row_stride_h, row_stride_t;         /* plain rows [batch, n_kv_heads, rows, head_dim], elements */
+} wkv_quantized_shape;
+
+/*
+ * Rows into caches, in all layers of a group: cache row first[b,h] + r becomes plain row tok_idx[b,h,r] (NULL: row r), for
+ * r < n_keep[b,h] (NULL: n_rows; at most n_rows).  With the tok_idx and n_keep of wkv_topk_windows it is what wkv_gather_group does, into fewer bits.
+ *   n_layers               1 .. WKV_MAX_LAYERS
+ *   k_layers, v_layers     host arrays [n_layers] of device pointers to plain rows, 16-byte aligned
+ *   tok_idx                device int32 [batch, n_kv_heads, n_rows], contiguous, or NULL
+ *   n_keep, first          device int32 [batch, n_kv_heads], or NULL (first: 0).  first is not changed: a caller that appends adds to its counts itself
+ *   k_codes, k_scales,
+ *   v_codes, v_scales      host arrays [n_layers] of device pointers; codes 16-byte, scales 4-byte aligned
+ * Cache rows outside 0 .. capacity - 1 and rows whose tok_idx is outside 0 .. row_capacity - 1 are not written; all others keep what they held.
+ */
+wkv_status wkv_cache_quantize(const wkv_quantized_shape *shape, int32_t n_layers, const void *const *k_layers, const void *const *v_layers,
+                              const int32_t *tok_idx, const int32_t *n_keep, const int32_t *first, void *const *k_codes, void *const *k_scales,
+                              void *const *v_codes, void *const *v_scales, void *hip_stream);
+
+/*
+ * And back: row r < n_rows of the outputs becomes what cache row first[b,h] + r stands for, where that row is below n_valid[b,h] (NULL: capacity);
+ * other rows are left as they are.  E.g. for wkv_prefill_attention over what a cache holds, or to go back to plain caches.  Values
+ * are exact in bf16 and fp32; fp16 rounds them once, and those past its largest number become that.
+ */
+wkv_status wkv_cache_dequantize(const wkv_quantized_shape *shape, int32_t n_layers, const void *const *k_codes, const void *const *k_scales,
+                                const void *const *v_codes, const void *const *v_scales, const int32_t *first, const int32_t *n_valid,
+                                void *const *k_out, void *const *v_out, void *hip_stream);
+
+/*
+ * wkv_decode_step over caches in 8 or 4 bits: the new token's rows are appended as wkv_cache_quantize holds them, and attention runs over what the
+ * caches then stand for.  q_new [batch, n_q_heads, head_dim] and k_new, v_new [batch, n_kv_heads, head_dim] contiguous, 16-byte
+ * aligned; n_valid, out and a (b, h) that cannot take the new row as at wkv_decode_step.  Workspace: 256-byte aligned, contents on entry irrelevant; calls that
+ * may overlap in time need workspaces of their own.
+ */
+size_t wkv_decode_quantized_workspace_bytes(const wkv_quantized_shape *shape);
+wkv_status wkv_decode_step_quantized(const wkv_quantized_shape *shape, const void *q_new, const void *k_new, const void *v_new,
+                                     void *k_codes, void *k_scales, void *v_codes, void *v_scales, int32_t *n_valid, float *out,
+                                     void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Attention for a tree of drafted tokens over a cache.  A sequence has n_nodes nodes; node t hangs below node parent[b,t] < t, or with -1
+ * below the last row of the cache.  Their keys and values are put into cache rows n .. n + n_nodes - 1, n = n_valid[b,h], node t into row n + t, and the query
+ * heads of node t attend to rows 0 .. n - 1, to the rows of the nodes it hangs below, up to the top, and to its own:
+ *     out[b,hq,t] = softmax(scale * q . K^T) . V   over these rows
+ * A node whose parent is anything else (padding) does not exist, nor does one below it: its row of out and its cache rows are left as they were.  n_valid is not
+ * changed: wkv_tree_accept keeps one path of the tree.  A chain of tokens has parent[t] = t - 1.
+ */
+#define WKV_MAX_NODES 64
+typedef struct {
+  int32_t batch;             /* >= 1; batch * n_kv_heads <= 65535                               */
+  int32_t n_q_heads;         /* multiple of n_kv_heads, at most 8 query heads per KV head       */
+  int32_t n_kv_heads;
+  int32_t head_dim;          /* 64 or 128                                                       */
+  int32_t dtype;             /* wkv_dtype of all tensors, out among them                        */
+  float   scale;             /* logit scale; 0 selects 1/sqrt(head_dim)                         */
+  int32_t n_nodes;           /* 1 .. WKV_MAX_NODES                                              */
+  int32_t capacity;          /* rows per (b, h) in the caches, at most 2^30                      */
+  int64_t cache_stride_b, cache_stride_h, cache_stride_t;   /* elements; head_dim contiguous; 64 rows of a cache are less than 2 GiB apart */
+  int64_t q_stride_b, q_stride_h, q_stride_t;               /* q_new [batch, n_q_heads, n_nodes, head_dim]  */
+  int64_t new_stride_b, new_stride_h, new_stride_t;         /* k_new, v_new [batch, n_kv_heads, n_nodes, head_dim] */
+  int64_t out_stride_b, out_stride_h, out_stride_t;         /* out as q_new                                 */
+  int32_t flags;             /* 0, or WKV_DECODE_KEEP_COUNT (wkv_tree_accept)                   */
+} wkv_tree_shape;
+
+/*
+ *   q_new, k_new, v_new    device, 16-byte aligned, e.g. the heads of one fused projection by their strides
+ *   parent                 device int32 [batch, n_nodes], contiguous
+ *   k_cache, v_cache       device [batch, n_kv_heads, capacity, head_dim]; rows 0 .. n - 1 must be finite, others may hold anything
+ *   n_valid                device int32 [batch, n_kv_heads]; read
+ *   out                    device; must not overlap the inputs, nor a row another row
+ * A (b, h) whose n_valid is negative or leaves no room for n_nodes rows keeps its caches; out is NaN for the nodes that exist.  Where a node's new value row holds an
+ * infinity or a NaN, the rows of out of the nodes that attend to it are NaN, and no others; what padding holds shows nowhere.
+ * Logits, softmax and sums are fp32; probabilities are rounded as at wkv_prefill_attention.  Workspace as at wkv_decode_step_quantized.
+ */
+size_t wkv_tree_workspace_bytes(const wkv_tree_shape *shape);
+wkv_status wkv_decode_tree(const wkv_tree_shape *shape, const void *q_new, const void *k_new, const void *v_new, const int32_t *parent,
+                           void *k_cache, void *v_cache, const int32_t *n_valid, void *out, void *workspace, size_t workspace_bytes,
+                           void *hip_stream);
+
+/*
+ * Keeps the first n_accept[b] nodes of path[b] and forgets the others of the tree, in all layers that share their row counts: cache row n + path[b,i] becomes row
+ * n + i, and n_valid[b,h] grows by as much (with WKV_DECODE_KEEP_COUNT it is left, for all but the last of several calls).
+ *   shape                the tree's (q, new and out strides and scale are not used, but must be valid)
+ *   n_layers             1 .. WKV_MAX_LAYERS
+ *   k_caches, v_caches   host arrays [n_layers] of device pointers; in place
+ *   path                 device int32 [batch, n_nodes]: node numbers, strictly ascending as a path from the top is; entries past n_accept[b] are not read
+ *   n_accept             device int32 [batch], 0 .. n_nodes
+ *   n_valid              device int32 [batch, n_kv_heads]
+ * A path is taken as far as it ascends within 0 .. n_nodes - 1.  A (b, h) that could not take the tree is left as it is.  The rows behind the new count hold what they held.
+ */
+wkv_status wkv_tree_accept(const wkv_tree_shape *shape, int32_t n_layers, void *const *k_caches, void *const *v_caches, const int32_t *path,
+                           const int32_t *n_accept, int32_t *n_valid, void *hip_stream);
+
 const char *wkv_status_string(wkv_status status);
 
 /* Message describing the most recent failure on the calling thread ("" if none). */

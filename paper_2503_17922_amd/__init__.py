@@ -23,6 +23,9 @@ WKV_SCORE_TWO_PASS, WKV_SCORE_SINGLE_READ, WKV_DEBUG_WAIT_GIVES_UP = 2, 4, 8    
 WKV_DECODE_KEEP_COUNT = 1     # DecodeShape(flags=...): n_valid is read but not advanced
 WKV_ROPE_INTERLEAVED, WKV_ROPE_INVERSE = 1, 2                                    # RopeShape(interleaved=..., inverse=...)
 WKV_ROPE_PLAIN, WKV_ROPE_LINEAR, WKV_ROPE_BASE, WKV_ROPE_PARTS, WKV_ROPE_WAVELENGTH = 0, 1, 2, 3, 4     # wkv_rope_frequencies
+WKV_ROPE_MAX_AXES = 4
+WKV_CACHE_E4M3, WKV_CACHE_E2M1 = 0, 1                                            # QuantizedShape(format=...)
+WKV_MAX_NODES = 64
 WKV_MAX_BATCH, WKV_MAX_GROUPS, WKV_MAX_LAYERS, WKV_MAX_WIN = 64, 64, 64, 128
 WKV_MAX_OBS_ROWS, WKV_MAX_WINDOWS = 256, 32768
 WKV_N_STAGES = 4
@@ -33,7 +36,9 @@ EXPORTS = ("wkv_get_dims", "wkv_workspace_bytes", "wkv_get_workspace_layout", "w
            "wkv_compress_groups_profiled", "wkv_group_budgets", "wkv_status_string", "wkv_last_error",
            "wkv_decode_workspace_bytes", "wkv_decode_step", "wkv_decode_step_static", "wkv_index_jaccard",
            "wkv_rope", "wkv_rope_frequencies", "wkv_attention_workspace_bytes", "wkv_prefill_attention",
-           "wkv_decode_weighted_workspace_bytes", "wkv_decode_step_weighted", "wkv_evict_workspace_bytes", "wkv_cache_evict")
+           "wkv_decode_weighted_workspace_bytes", "wkv_decode_step_weighted", "wkv_evict_workspace_bytes", "wkv_cache_evict",
+           "wkv_norm_rope", "wkv_cache_quantize", "wkv_cache_dequantize", "wkv_decode_quantized_workspace_bytes", "wkv_decode_step_quantized",
+           "wkv_tree_workspace_bytes", "wkv_decode_tree", "wkv_tree_accept")
 WKV_DECODE_STATIC_SCRATCH_BYTES = 8 << 20
 
 
@@ -78,6 +83,24 @@ class _AttentionShape(C.Structure):
                [(f"{t}_stride_{x}", C.c_int64) for t in ("q", "kv", "out") for x in "bht"]
 
 
+class _NormRopeShape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "n_tokens", "n_q_heads", "n_kv_heads", "head_dim", "rotary_dim", "dtype", "flags", "n_axes")] + \
+               [("eps", C.c_float), ("amplitude", C.c_double), ("inv_freq", C.POINTER(C.c_double)), ("axis_of_pair", C.POINTER(C.c_int32))] + \
+               [(f"{t}_stride_{x}", C.c_int64) for t in ("q", "q_out", "k", "k_out") for x in "bht"]
+
+
+class _QuantizedShape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "n_q_heads", "n_kv_heads", "head_dim", "dtype", "format")] + \
+               [("scale", C.c_float), ("capacity", C.c_int32)] + [(f"code_stride_{x}", C.c_int64) for x in "bht"] + \
+               [(n, C.c_int32) for n in ("flags", "n_rows", "row_capacity")] + [(f"row_stride_{x}", C.c_int64) for x in "bht"]
+
+
+class _TreeShape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("batch", "n_q_heads", "n_kv_heads", "head_dim", "dtype")] + \
+               [("scale", C.c_float), ("n_nodes", C.c_int32), ("capacity", C.c_int32)] + \
+               [(f"{t}_stride_{x}", C.c_int64) for t in ("cache", "q", "new", "out") for x in "bht"] + [("flags", C.c_int32)]
+
+
 class Dims(C.Structure):
     _fields_ = [("obs_rows", C.c_int32), ("t_stride", C.c_int32), ("nw_max", C.c_int32),
                 ("k_max", C.c_int32), ("nkeep_max", C.c_int32), ("total_tokens", C.c_int64)]
@@ -98,7 +121,7 @@ def native():
         lib()
         module = importlib.import_module("._native", __name__)
         module.bind(_current_stream, _structure, Problem, _Problem, DecodeShape, _DecodeShape, RopeShape, _RopeShape,
-                    AttentionShape, _AttentionShape)
+                    AttentionShape, _AttentionShape, NormRopeShape, _NormRopeShape, QuantizedShape, _QuantizedShape, TreeShape, _TreeShape)
         _calls = module
     return _calls
 
@@ -164,6 +187,15 @@ def lib() -> C.CDLL:
     l.wkv_decode_step_weighted.argtypes = [DP] + [VP] * 11 + [SZ, VP]; l.wkv_decode_step_weighted.restype = C.c_int
     l.wkv_evict_workspace_bytes.argtypes = [DP]; l.wkv_evict_workspace_bytes.restype = SZ
     l.wkv_cache_evict.argtypes = [DP, C.c_int32, VPP, VPP, VP, VP, VP, VP, C.c_int32, VP, SZ, VP]; l.wkv_cache_evict.restype = C.c_int
+    NP, QP, TP = C.POINTER(_NormRopeShape), C.POINTER(_QuantizedShape), C.POINTER(_TreeShape)
+    l.wkv_norm_rope.argtypes = [NP] + [VP] * 8; l.wkv_norm_rope.restype = C.c_int
+    l.wkv_cache_quantize.argtypes = [QP, C.c_int32, VPP, VPP, VP, VP, VP, VPP, VPP, VPP, VPP, VP]; l.wkv_cache_quantize.restype = C.c_int
+    l.wkv_cache_dequantize.argtypes = [QP, C.c_int32, VPP, VPP, VPP, VPP, VP, VP, VPP, VPP, VP]; l.wkv_cache_dequantize.restype = C.c_int
+    l.wkv_decode_quantized_workspace_bytes.argtypes = [QP]; l.wkv_decode_quantized_workspace_bytes.restype = SZ
+    l.wkv_decode_step_quantized.argtypes = [QP] + [VP] * 10 + [SZ, VP]; l.wkv_decode_step_quantized.restype = C.c_int
+    l.wkv_tree_workspace_bytes.argtypes = [TP]; l.wkv_tree_workspace_bytes.restype = SZ
+    l.wkv_decode_tree.argtypes = [TP] + [VP] * 9 + [SZ, VP]; l.wkv_decode_tree.restype = C.c_int
+    l.wkv_tree_accept.argtypes = [TP, C.c_int32, VPP, VPP, VP, VP, VP, VP]; l.wkv_tree_accept.restype = C.c_int
     l.wkv_status_string.argtypes = [C.c_int]; l.wkv_status_string.restype = C.c_char_p
     l.wkv_last_error.argtypes = []; l.wkv_last_error.restype = C.c_char_p
     _lib = l
@@ -442,3 +474,104 @@ def wkv_evict_workspace_bytes(shape: DecodeShape) -> int:
 def wkv_cache_evict(shape: DecodeShape, k_caches, v_caches, weights, tok_idx, n_valid, keep, recent, workspace, stream=None) -> None:
     """``k_caches``, ``v_caches``: the caches of the layers that share the row counts."""
     _check((_calls or native()).cache_evict(shape, k_caches, v_caches, weights, tok_idx, n_valid, keep, recent, workspace, stream))
+
+
+class NormRopeShape:
+    """Mirrors ``wkv_norm_rope_shape``.  Strides (b, h, t) in elements; ``None`` selects contiguous ``[B, H, T, d]`` tensors, for
+    the outputs the strides of the inputs.  ``axis_of_pair``: for every pair of channels the axis whose position turns it, ``None``: the first."""
+
+    def __init__(self, *, batch: int, n_tokens: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int,
+                 inv_freq: Sequence[float], n_axes: int = 1, axis_of_pair: Optional[Sequence[int]] = None, eps: float = 1e-6,
+                 amplitude: float = 1.0, interleaved: bool = False, q_strides=None, k_strides=None, q_out_strides=None, k_out_strides=None):
+        d = head_dim
+        rows = max(n_tokens, 1)
+        if axis_of_pair is not None and len(axis_of_pair) != len(inv_freq):
+            raise ValueError(f"axis_of_pair has {len(axis_of_pair)} entries, inv_freq {len(inv_freq)}")
+        q_strides = q_strides or (n_q_heads * rows * d, rows * d, d)
+        k_strides = k_strides or (n_kv_heads * rows * d, rows * d, d)
+        self._keep = [(C.c_double * max(len(inv_freq), 1))(*inv_freq), _i32(axis_of_pair) if axis_of_pair is not None else None]
+        self.c = _NormRopeShape(batch, n_tokens, n_q_heads, n_kv_heads, d, 2 * len(inv_freq), dtype, WKV_ROPE_INTERLEAVED if interleaved else 0,
+                                n_axes, eps, amplitude, *self._keep, *q_strides, *(q_out_strides or q_strides), *k_strides,
+                                *(k_out_strides or k_strides))
+
+    def ref(self):
+        return C.byref(self.c)
+
+
+def wkv_norm_rope(shape: NormRopeShape, positions, q_weight, k_weight, q_in, q_out, k_in, k_out, stream=None) -> None:
+    """``positions``: int32 [batch, n_tokens, n_axes]; ``q_weight``, ``k_weight``: [head_dim] of the tensors' type, or None."""
+    _check((_calls or native()).norm_rope(shape, positions, q_weight, k_weight, q_in, q_out, k_in, k_out, stream))
+
+
+class QuantizedShape:
+    """Mirrors ``wkv_quantized_shape``.  ``code_strides`` in bytes, ``None``: contiguous codes ``[B, Hkv, capacity, bytes of a row]``; ``row_strides`` in
+    elements, ``None``: contiguous plain rows ``[B, Hkv, row_capacity, d]``.  ``row_capacity`` ``None``: ``n_rows``."""
+
+    def __init__(self, *, batch: int, n_kv_heads: int, head_dim: int, dtype: int, format: int, capacity: int, n_q_heads: Optional[int] = None,
+                 scale: float = 0.0, code_strides=None, n_rows: int = 0, row_capacity: Optional[int] = None, row_strides=None, flags: int = 0):
+        row = head_dim if format == WKV_CACHE_E4M3 else head_dim // 2
+        row_capacity = n_rows if row_capacity is None else row_capacity
+        rows = max(row_capacity, 1)
+        code_strides = code_strides or (n_kv_heads * capacity * row, capacity * row, row)
+        row_strides = row_strides or (n_kv_heads * rows * head_dim, rows * head_dim, head_dim)
+        self.c = _QuantizedShape(batch, n_kv_heads if n_q_heads is None else n_q_heads, n_kv_heads, head_dim, dtype, format, scale, capacity,
+                                 *code_strides, flags, n_rows, row_capacity, *row_strides)
+
+    def ref(self):
+        return C.byref(self.c)
+
+
+def wkv_cache_quantize(shape: QuantizedShape, k_layers, v_layers, tok_idx, n_keep, first, k_codes, k_scales, v_codes, v_scales, stream=None) -> None:
+    """``k_layers`` ... ``v_scales``: a tensor for every layer; ``tok_idx``, ``n_keep``, ``first``: int32, or None."""
+    _check((_calls or native()).cache_quantize(shape, k_layers, v_layers, tok_idx, n_keep, first, k_codes, k_scales, v_codes, v_scales, stream))
+
+
+def wkv_cache_dequantize(shape: QuantizedShape, k_codes, k_scales, v_codes, v_scales, first, n_valid, k_out, v_out, stream=None) -> None:
+    _check((_calls or native()).cache_dequantize(shape, k_codes, k_scales, v_codes, v_scales, first, n_valid, k_out, v_out, stream))
+
+
+def wkv_decode_quantized_workspace_bytes(shape: QuantizedShape) -> int:
+    n = lib().wkv_decode_quantized_workspace_bytes(shape.ref())
+    if n == 0:
+        raise WkvError(WKV_ERR_INVALID_ARG, lib().wkv_last_error().decode())
+    return int(n)
+
+
+def wkv_decode_step_quantized(shape: QuantizedShape, q_new, k_new, v_new, k_codes, k_scales, v_codes, v_scales, n_valid, out, workspace,
+                              stream=None) -> None:
+    _check((_calls or native()).decode_step_quantized(shape, q_new, k_new, v_new, k_codes, k_scales, v_codes, v_scales, n_valid, out, workspace,
+                                                      stream))
+
+
+class TreeShape:
+    """Mirrors ``wkv_tree_shape``.  Strides (b, h, t) in elements; ``None`` selects contiguous caches ``[B, Hkv, capacity, d]`` and contiguous
+    ``[B, H, n_nodes, d]`` for the others (``out_strides``: ``q_strides``)."""
+
+    def __init__(self, *, batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int, n_nodes: int, capacity: int,
+                 scale: float = 0.0, cache_strides=None, q_strides=None, new_strides=None, out_strides=None, flags: int = 0):
+        d = head_dim
+        cache_strides = cache_strides or (n_kv_heads * capacity * d, capacity * d, d)
+        q_strides = q_strides or (n_q_heads * n_nodes * d, n_nodes * d, d)
+        new_strides = new_strides or (n_kv_heads * n_nodes * d, n_nodes * d, d)
+        self.c = _TreeShape(batch, n_q_heads, n_kv_heads, d, dtype, scale, n_nodes, capacity, *cache_strides, *q_strides, *new_strides,
+                            *(out_strides or q_strides), flags)
+
+    def ref(self):
+        return C.byref(self.c)
+
+
+def wkv_tree_workspace_bytes(shape: TreeShape) -> int:
+    n = lib().wkv_tree_workspace_bytes(shape.ref())
+    if n == 0:
+        raise WkvError(WKV_ERR_INVALID_ARG, lib().wkv_last_error().decode())
+    return int(n)
+
+
+def wkv_decode_tree(shape: TreeShape, q_new, k_new, v_new, parent, k_cache, v_cache, n_valid, out, workspace, stream=None) -> None:
+    """``parent``: int32 [batch, n_nodes]; -1: below the last row of the cache."""
+    _check((_calls or native()).decode_tree(shape, q_new, k_new, v_new, parent, k_cache, v_cache, n_valid, out, workspace, stream))
+
+
+def wkv_tree_accept(shape: TreeShape, k_caches, v_caches, path, n_accept, n_valid, stream=None) -> None:
+    """``k_caches``, ``v_caches``: the caches of the layers that share the row counts; ``path``: int32 [batch, n_nodes]."""
+    _check((_calls or native()).tree_accept(shape, k_caches, v_caches, path, n_accept, n_valid, stream))

@@ -14,56 +14,11 @@
 // 7.84 (4096 tokens 133 and 146 us).  No better: 64 rows a wave with a SIMD for itself, so that a fragment from LDS feeds two products (9.07; with the next tile's
 // logits computed beside this one's exponentials the registers do not suffice); a reference that moves when a tile's sum overflows, without
 // maxima (+2 %); 128 keys to a barrier (+4 %); three or four tiles in LDS (+1 %); wave priorities (the same).
-#include "wkv_device.h"
-#include "wkv_operators.h"
+#include "wkv_attention_tile.h"
 
 namespace wkv {
 
 namespace {
-
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
-
-template <int D_, int DT, int WAVES_>
-struct Att {
-  static constexpr int D = D_, ES = DT == DT_F32 ? 4 : 2;
-  static constexpr int WAVES = WAVES_, NT = WAVES * 64;
-  static constexpr int KEYS = att_tile_keys(DT == DT_F32);      // of a tile
-  static constexpr int KT = KEYS / 32;
-  static constexpr int ROWB = D * ES, PPR = ROWB / 16;      // bytes and 16-byte pieces of a row
-  static constexpr int KS = PPR / 2;                      // contraction steps over the channels, two pieces each
-  static constexpr int VT = D / 32;                       // channel tiles of the output
-  static constexpr int TILE = KEYS * ROWB, STAGE = 2 * TILE, STAGES = 2;
-  static constexpr int RPI = 64 / PPR;                    // rows of a DMA instruction
-  static constexpr int LPT = TILE / 1024 / WAVES;         // DMA instructions of a wave per tile of keys (of values)
-  static constexpr int OFFS = 16 / (RPI * WAVES) > 1 ? 16 / (RPI * WAVES) : 1;      // of them with key offsets of their own
-  // Where piece p of row r lies within its row's slot.  Keys are read by 32 lanes of as many rows, a piece each: rows 16 apart share a
-  // place.  Values: 16-bit types by four rows of 64 bytes at a time, fp32 by two rows, four apart, of 128 bytes.
-  static __device__ __forceinline__ int key_slot(int r, int p) { return p ^ (PPR == 8 ? (r >> 1) & 7 : r & 15); }
-  static __device__ __forceinline__ int value_slot(int r, int p) {
-    return p ^ (ES == 4 ? (r >> 2 & 1) * 8 : PPR == 8 ? (r >> 1 & 1) * 4 : (r & 3) * 4);
-  }
-};
-
-// A DMA instruction of a wave, from base + off bytes of each lane.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void dma_rows(uint32_t lds, const char *base, uint32_t off) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
-}
-#pragma clang diagnostic pop
-
-// Two floats as a pair of 16-bit numbers, each rounded to nearest.
-template <int DT>
-__device__ __forceinline__ uint32_t pack_pair(float a, float b) {
-  if constexpr (DT == DT_F16) {
-    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, (h2){(_Float16)a, (_Float16)b});
-  } else {
-    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, (b2){(__bf16)a, (__bf16)b});
-  }
-}
 
 // Which block of which (sequence, KV head) work item `item` is, and what follows for the keys.
 template <int ROWS>
@@ -93,14 +48,6 @@ struct Block {
 
 // Natural logarithm of a row's sum, from its base-2 reference; no key weighs anything: -inf.
 __device__ __forceinline__ float row_lse(float m, float l) { return l == 0.0f ? -INFINITY : (m + fast_log2(l)) * 0.69314718055994531f; }
-
-// A row's reference moves when a logit exceeds it by LIFT + GROW (base 2), to LIFT below that logit: the largest probability of a row is 2^LIFT to 2^(LIFT + GROW).
-// For the product with the values 16-bit types round a probability to their own type, by half a step: an fp32 product takes eight times as long.  (Their sum, which the
-// normaliser needs in fp32, is of the unrounded ones.)  fp16 has all its bits from 2^-14 to 2^16 alone and nothing below 2^-25, so its probabilities are held high: what
-// it loses of a key is at most 2^-38 of the row's sum, and of 8192 keys, with values up to 1, no more than the rounding of an output in fp16 does.  Unlifted, a key of value zero that
-// stands 17 (base e) above 4096 others left a third of the output wrong.  GROW of 0 / 1 / 2 / 4 / 8, the packed prompts of 17.4K tokens
-// in fp16: 940 / 924 / 914 / 905 / 905 us.
-template <int DT> struct Reference { static constexpr float LIFT = DT == DT_F16 ? 13.0f : 0.0f, GROW = DT == DT_F16 ? 2.0f : 8.0f; };
 
 // -inf for the normalisers of rows that do not exist, by the workgroup of the first block.
 template <int ROWS>

@@ -1,0 +1,294 @@
+// Host side of the operators of generation: argument validation, derived sizes, launch plans and the entry points.
+// Nothing in this file but the launchers' calls touches the GPU.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "wkv_generation.h"
+
+namespace wkv {
+
+namespace {
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+wkv_status plan_norm_rope(const wkv_norm_rope_shape *p, NormRopeArgs *a) {
+  set_error("");
+  if (!p) return invalid("shape is NULL");
+  if (p->batch < 1) { set_error("batch must be >= 1 (got %d)", p->batch); return WKV_ERR_INVALID_ARG; }
+  if (p->n_tokens < 0) return invalid("n_tokens must be >= 0");
+  if ((int64_t)p->batch * p->n_tokens > 1 << 25) { set_error("batch * n_tokens exceeds 2^25; split the call"); return WKV_ERR_UNSUPPORTED; }
+  if (p->n_q_heads < 0 || p->n_kv_heads < 0) return invalid("numbers of heads must be >= 0");
+  if (p->n_q_heads > 65535 || p->n_kv_heads > 65535) { set_error("more than 65535 heads"); return WKV_ERR_UNSUPPORTED; }
+  if (!known_dtype(p->dtype)) return WKV_ERR_INVALID_ARG;
+  if (p->head_dim != 64 && p->head_dim != 128) { set_error("head_dim %d is not supported (64 or 128)", p->head_dim); return WKV_ERR_UNSUPPORTED; }
+  if (p->rotary_dim < 1 || p->rotary_dim > p->head_dim) { set_error("rotary_dim %d outside [1, head_dim]", p->rotary_dim); return WKV_ERR_INVALID_ARG; }
+  if (p->rotary_dim % 16 != 0) { set_error("rotary_dim %d is not supported (a multiple of 16)", p->rotary_dim); return WKV_ERR_UNSUPPORTED; }
+  if (p->flags & ~WKV_ROPE_INTERLEAVED) { set_error("unknown bits in flags (0x%x)", p->flags); return WKV_ERR_INVALID_ARG; }
+  if (p->n_axes < 1 || p->n_axes > WKV_ROPE_MAX_AXES) { set_error("n_axes %d outside [1, %d]", p->n_axes, WKV_ROPE_MAX_AXES); return WKV_ERR_INVALID_ARG; }
+  if (!(p->eps >= 0.0f) || std::isinf(p->eps)) return invalid("eps must be finite and >= 0");
+  if (!std::isfinite(p->amplitude) || std::fabs(p->amplitude) > 3.0e38) return invalid("amplitude must be finite (0 selects 1)");
+  if (!p->inv_freq) return invalid("inv_freq must be a non-NULL host array");
+  for (int32_t i = 0; i < p->rotary_dim / 2; ++i) {
+    if (!std::isfinite(p->inv_freq[i])) { set_error("inv_freq[%d] is not finite", i); return WKV_ERR_INVALID_ARG; }
+    if (p->axis_of_pair && (p->axis_of_pair[i] < 0 || p->axis_of_pair[i] >= p->n_axes)) {
+      set_error("axis_of_pair[%d] = %d outside [0, %d)", i, p->axis_of_pair[i], p->n_axes); return WKV_ERR_INVALID_ARG;
+    }
+  }
+  if (p->n_q_heads && (!good_strides(p->dtype, p->head_dim, p->q_stride_b, p->q_stride_h, p->q_stride_t, "q") ||
+                       !good_strides(p->dtype, p->head_dim, p->q_out_stride_b, p->q_out_stride_h, p->q_out_stride_t, "q_out")))
+    return WKV_ERR_INVALID_ARG;
+  if (p->n_kv_heads && (!good_strides(p->dtype, p->head_dim, p->k_stride_b, p->k_stride_h, p->k_stride_t, "k") ||
+                        !good_strides(p->dtype, p->head_dim, p->k_out_stride_b, p->k_out_stride_h, p->k_out_stride_t, "k_out")))
+    return WKV_ERR_INVALID_ARG;
+  std::memset(a, 0, sizeof(*a));
+  const int64_t e = elem_bytes(p->dtype);
+  a->q = {nullptr, nullptr, p->q_stride_b * e, p->q_stride_h * e, p->q_stride_t * e, p->q_out_stride_b * e, p->q_out_stride_h * e, p->q_out_stride_t * e};
+  a->k = {nullptr, nullptr, p->k_stride_b * e, p->k_stride_h * e, p->k_stride_t * e, p->k_out_stride_b * e, p->k_out_stride_h * e, p->k_out_stride_t * e};
+  for (int32_t i = 0; i < p->rotary_dim / 2; ++i) {
+    a->turns[i] = turns_of(p->inv_freq[i]);
+    a->axis[i] = (uint8_t)(p->axis_of_pair ? p->axis_of_pair[i] : 0);
+  }
+  a->batch = p->batch; a->n_tokens = p->n_tokens; a->q_heads = p->n_q_heads; a->kv_heads = p->n_kv_heads;
+  a->d = p->head_dim; a->rotary = p->rotary_dim; a->dtype = p->dtype; a->n_axes = p->n_axes;
+  a->interleaved = (p->flags & WKV_ROPE_INTERLEAVED) ? 1 : 0;
+  a->amplitude = p->amplitude == 0.0 ? 1.0f : (float)p->amplitude;
+  a->eps = p->eps;
+  return WKV_OK;
+}
+
+// The checks of caches in 8 and 4 bits; key ranges and partial results of a decode step are those of plain caches.
+wkv_status plan_quantized(const wkv_quantized_shape *p, Decode *dc) {
+  set_error("");
+  if (!p) return invalid("shape is NULL");
+  wkv_decode_shape s;
+  std::memset(&s, 0, sizeof s);
+  s.batch = p->batch; s.n_q_heads = p->n_q_heads; s.n_kv_heads = p->n_kv_heads; s.head_dim = p->head_dim; s.dtype = p->dtype; s.scale = p->scale;
+  s.capacity = p->capacity; s.flags = p->flags;
+  s.cache_stride_b = s.cache_stride_h = s.cache_stride_t = 128;                    // (the codes' own are checked below)
+  const wkv_status st = validate_decode(&s, dc);
+  if (st != WKV_OK) return st;
+  if (p->format != WKV_CACHE_E4M3 && p->format != WKV_CACHE_E2M1) { set_error("unknown format %d", p->format); return WKV_ERR_INVALID_ARG; }
+  if (p->capacity > 1 << 30) { set_error("capacity %d is not supported (at most 2^30 rows)", p->capacity); return WKV_ERR_UNSUPPORTED; }
+  const int64_t row = p->format == WKV_CACHE_E4M3 ? p->head_dim : p->head_dim / 2;
+  const int64_t strides[3] = {p->code_stride_b, p->code_stride_h, p->code_stride_t};
+  for (const int64_t x : strides)
+    if (x < 0 || x % 16 != 0 || x > MAX_STRIDE) return invalid("code strides must be non-negative multiples of 16 bytes, at most 2^48");
+  if (p->code_stride_t < row || p->code_stride_h < row) { set_error("code token and head strides must be >= %lld bytes", (long long)row); return WKV_ERR_INVALID_ARG; }
+  // (the rows of a block are addressed by 32-bit offsets)
+  if (p->code_stride_t * 32 > 0x7fffffff) { set_error("code token stride %lld is not supported", (long long)p->code_stride_t); return WKV_ERR_UNSUPPORTED; }
+  dc->shape.sb = p->code_stride_b; dc->shape.sh = p->code_stride_h; dc->shape.st = p->code_stride_t;
+  return WKV_OK;
+}
+
+// Rows in and out of caches: checks, and everything of the launch but the pointers of the counts.
+wkv_status plan_rows(const wkv_quantized_shape *p, int32_t n_layers, const void *const *k_plain, const void *const *v_plain, const void *const *k_codes,
+                     const void *const *k_scales, const void *const *v_codes, const void *const *v_scales, QuantizedArgs *a, QuantizedLayers *layers) {
+  Decode dc;
+  const wkv_status st = plan_quantized(p, &dc);
+  if (st != WKV_OK) return st;
+  if (p->n_rows < 0) return invalid("n_rows must be >= 0");
+  const DecodeShape &s = dc.shape;
+  if ((int64_t)s.B * s.Hkv * p->n_rows > 1 << 30) { set_error("batch * n_kv_heads * n_rows exceeds 2^30; split the call"); return WKV_ERR_UNSUPPORTED; }
+  if (!good_strides(p->dtype, p->head_dim, p->row_stride_b, p->row_stride_h, p->row_stride_t, "row")) return WKV_ERR_INVALID_ARG;
+  if (n_layers < 1 || n_layers > WKV_MAX_LAYERS) { set_error("n_layers outside [1, %d]", WKV_MAX_LAYERS); return WKV_ERR_INVALID_ARG; }
+  if (!k_plain || !v_plain || !k_codes || !k_scales || !v_codes || !v_scales) return invalid("an array of layers is NULL");
+  std::memset(a, 0, sizeof *a);
+  std::memset(layers, 0, sizeof *layers);
+  for (int32_t l = 0; l < n_layers; ++l) {
+    layers->plain[0][l] = k_plain[l]; layers->plain[1][l] = v_plain[l];
+    layers->codes[0][l] = k_codes[l]; layers->codes[1][l] = v_codes[l];
+    layers->scales[0][l] = k_scales[l]; layers->scales[1][l] = v_scales[l];
+    for (int i = 0; i < 2; ++i) {
+      if (!layers->plain[i][l] || !layers->codes[i][l] || !layers->scales[i][l]) { set_error("a tensor of layer %d is NULL", l); return WKV_ERR_INVALID_ARG; }
+      if (misaligned(layers->plain[i][l], 16) || misaligned(layers->codes[i][l], 16)) { set_error("rows and codes of layer %d must be 16-byte aligned", l); return WKV_ERR_INVALID_ARG; }
+      if (misaligned(layers->scales[i][l], 4)) { set_error("scales of layer %d must be 4-byte aligned", l); return WKV_ERR_INVALID_ARG; }
+    }
+  }
+  const int64_t e = elem_bytes(p->dtype);
+  a->heads = s.B * s.Hkv; a->Hkv = s.Hkv; a->d = s.d; a->dtype = s.dtype; a->format = p->format;
+  a->capacity = s.capacity; a->n_rows = p->n_rows; a->row_capacity = p->row_capacity; a->kv_magic = s.kv_magic;
+  a->c_sb = s.sb; a->c_sh = s.sh; a->c_st = s.st;
+  a->r_sb = p->row_stride_b * e; a->r_sh = p->row_stride_h * e; a->r_st = p->row_stride_t * e;
+  return WKV_OK;
+}
+
+}  // namespace
+
+// How the work is cut: blocks of 32 to 256 rows, and ranges of a cache so that about 1024 workgroups have work if every cache is full.
+wkv_status plan_tree(const wkv_tree_shape *p, TreePlan *plan) {
+  set_error("");
+  if (!p) return invalid("shape is NULL");
+  if (p->batch < 1) { set_error("batch must be >= 1 (got %d)", p->batch); return WKV_ERR_INVALID_ARG; }
+  if (p->n_kv_heads < 1 || p->n_q_heads < 1 || p->n_q_heads % p->n_kv_heads != 0) {
+    set_error("n_q_heads (%d) must be a positive multiple of n_kv_heads (%d)", p->n_q_heads, p->n_kv_heads); return WKV_ERR_INVALID_ARG;
+  }
+  if ((int64_t)p->batch * p->n_kv_heads > 65535) { set_error("batch * n_kv_heads exceeds 65535 (launch grid limit); split the call"); return WKV_ERR_UNSUPPORTED; }
+  const int32_t G = p->n_q_heads / p->n_kv_heads;
+  if (G > 8) { set_error("n_q_heads / n_kv_heads = %d is not supported (at most 8)", G); return WKV_ERR_UNSUPPORTED; }
+  if (!known_dtype(p->dtype)) return WKV_ERR_INVALID_ARG;
+  if (p->head_dim != 64 && p->head_dim != 128) { set_error("head_dim %d is not supported (64 or 128)", p->head_dim); return WKV_ERR_UNSUPPORTED; }
+  if (!(p->scale >= 0.0f) || std::isinf(p->scale)) return invalid("scale must be finite and >= 0 (0 selects 1/sqrt(head_dim))");
+  if (p->n_nodes < 1) { set_error("n_nodes must be >= 1 (got %d)", p->n_nodes); return WKV_ERR_INVALID_ARG; }
+  if (p->n_nodes > WKV_MAX_NODES) { set_error("n_nodes %d exceeds WKV_MAX_NODES=%d", p->n_nodes, WKV_MAX_NODES); return WKV_ERR_UNSUPPORTED; }
+  if (p->capacity < 1) return invalid("capacity must be >= 1");
+  if (p->capacity > 1 << 30) { set_error("capacity %d is not supported (at most 2^30 rows)", p->capacity); return WKV_ERR_UNSUPPORTED; }
+  if (p->flags & ~WKV_DECODE_KEEP_COUNT) { set_error("unknown bits in flags (0x%x)", p->flags); return WKV_ERR_INVALID_ARG; }
+  if (!good_strides(p->dtype, p->head_dim, p->cache_stride_b, p->cache_stride_h, p->cache_stride_t, "cache") ||
+      !good_strides(p->dtype, p->head_dim, p->q_stride_b, p->q_stride_h, p->q_stride_t, "q") ||
+      !good_strides(p->dtype, p->head_dim, p->new_stride_b, p->new_stride_h, p->new_stride_t, "new") ||
+      !good_strides(p->dtype, p->head_dim, p->out_stride_b, p->out_stride_h, p->out_stride_t, "out"))
+    return WKV_ERR_INVALID_ARG;
+  // (the rows that a wave fetches of a tile are addressed by 32-bit offsets)
+  if (p->cache_stride_t * elem_bytes(p->dtype) * 64 > 0x7fffffff) { set_error("cache token stride %lld is not supported", (long long)p->cache_stride_t); return WKV_ERR_UNSUPPORTED; }
+  std::memset(plan, 0, sizeof *plan);
+  TreeArgs &a = plan->args;
+  const bool f32 = p->dtype == WKV_F32;
+  a.heads = p->batch * p->n_kv_heads; a.Hkv = p->n_kv_heads; a.G = G; a.d = p->head_dim; a.dtype = p->dtype; a.T = p->n_nodes; a.capacity = p->capacity;
+  a.n_rows = a.T * G;
+  a.heads_magic = division_magic(a.heads); a.kv_magic = division_magic(a.Hkv); a.g_magic = division_magic(G);
+  const double scale = p->scale > 0.0f ? (double)p->scale : 1.0 / std::sqrt((double)p->head_dim);
+  a.c1 = (float)(scale * 1.4426950408889634074);
+  const int64_t e = elem_bytes(p->dtype);
+  a.c_sb = p->cache_stride_b * e; a.c_sh = p->cache_stride_h * e; a.c_st = p->cache_stride_t * e;
+  a.q_sb = p->q_stride_b * e; a.q_sh = p->q_stride_h * e; a.q_st = p->q_stride_t * e;
+  a.n_sb = p->new_stride_b * e; a.n_sh = p->new_stride_h * e; a.n_st = p->new_stride_t * e;
+  a.o_sb = p->out_stride_b * e; a.o_sh = p->out_stride_h * e; a.o_st = p->out_stride_t * e;
+  // fp32 tiles are twice as large: two key waves at most, and blocks of 128 rows
+  plan->row_waves = a.n_rows <= 32 && !f32 ? 1 : a.n_rows <= 64 ? 2 : a.n_rows <= 128 || f32 ? 4 : 8;
+  plan->key_waves = plan->row_waves == 1 ? 4 : plan->row_waves == 2 ? 2 : 1;
+  const int32_t rows = plan->row_waves * 32, keys = tree_wave_keys(f32, plan->key_waves) * plan->key_waves;
+  a.blocks = (int32_t)ceil_div(a.n_rows, rows);
+  const int64_t tiles = ceil_div(p->capacity, keys);
+  const int64_t want = std::max<int64_t>(1024 / ((int64_t)a.heads * a.blocks), 1);
+  a.chunk = (int32_t)std::max<int64_t>(ceil_div(tiles, want), ceil_div(128, keys));
+  a.splits = (int32_t)ceil_div(tiles, a.chunk);
+  plan->ws_bytes = 256;
+  if (a.splits > 1) {
+    const size_t all = (size_t)a.heads * a.blocks * a.splits * rows;
+    plan->stats_at = all * a.d * sizeof(float);
+    plan->ws_bytes = round_up(plan->stats_at + all * sizeof(float2));
+  }
+  return WKV_OK;
+}
+
+}  // namespace wkv
+
+using namespace wkv;
+
+extern "C" {
+
+wkv_status wkv_norm_rope(const wkv_norm_rope_shape *shape, const int32_t *positions, const void *q_weight, const void *k_weight, const void *q_in,
+                         void *q_out, const void *k_in, void *k_out, void *hip_stream) {
+  NormRopeArgs a;
+  const wkv_status st = plan_norm_rope(shape, &a);
+  if (st != WKV_OK) return st;
+  if (a.n_tokens == 0 || (a.q_heads == 0 && a.kv_heads == 0)) return WKV_OK;
+  if (!positions) return invalid("positions is NULL");
+  if (misaligned(positions, 4)) return invalid("positions must be 4-byte aligned");
+  if (a.q_heads && (!q_in || !q_out)) return invalid("q_in / q_out is NULL");
+  if (a.kv_heads && (!k_in || !k_out)) return invalid("k_in / k_out is NULL");
+  if ((a.q_heads && (misaligned(q_in, 16) || misaligned(q_out, 16) || misaligned(q_weight, 16))) ||
+      (a.kv_heads && (misaligned(k_in, 16) || misaligned(k_out, 16) || misaligned(k_weight, 16))))
+    return invalid("the tensors and weights must be 16-byte aligned");
+  a.q.in = q_in; a.q.out = q_out; a.k.in = k_in; a.k.out = k_out;
+  for (const RopeTensor *t : {a.q_heads ? &a.q : nullptr, a.kv_heads ? &a.k : nullptr})
+    if (t && t->in == t->out && (t->in_b != t->out_b || t->in_h != t->out_h || t->in_t != t->out_t))
+      return invalid("in place, input and output strides must be the same");
+  if (a.q_heads && a.kv_heads && q_out == k_out) return invalid("q_out and k_out are the same memory");
+  a.positions = positions;
+  a.q_weight = a.q_heads ? q_weight : nullptr; a.k_weight = a.kv_heads ? k_weight : nullptr;
+  return launched(launch_norm_rope(a, (hipStream_t)hip_stream), "wkv_norm_rope");
+}
+
+wkv_status wkv_cache_quantize(const wkv_quantized_shape *shape, int32_t n_layers, const void *const *k_layers, const void *const *v_layers,
+                              const int32_t *tok_idx, const int32_t *n_keep, const int32_t *first, void *const *k_codes, void *const *k_scales,
+                              void *const *v_codes, void *const *v_scales, void *hip_stream) {
+  QuantizedArgs a;
+  QuantizedLayers layers;
+  const wkv_status st = plan_rows(shape, n_layers, k_layers, v_layers, k_codes, k_scales, v_codes, v_scales, &a, &layers);
+  if (st != WKV_OK) return st;
+  if (shape->row_capacity < (tok_idx ? 0 : a.n_rows)) return invalid("row_capacity must be >= n_rows, or >= 0 with tok_idx");
+  if (misaligned(tok_idx, 4) || misaligned(n_keep, 4) || misaligned(first, 4)) return invalid("tok_idx, n_keep and first must be 4-byte aligned");
+  a.tok_idx = tok_idx; a.n_keep = n_keep; a.first = first;
+  if (a.n_rows == 0) return WKV_OK;
+  return launched(launch_quantize(a, layers, n_layers, (hipStream_t)hip_stream), "wkv_cache_quantize");
+}
+
+wkv_status wkv_cache_dequantize(const wkv_quantized_shape *shape, int32_t n_layers, const void *const *k_codes, const void *const *k_scales,
+                                const void *const *v_codes, const void *const *v_scales, const int32_t *first, const int32_t *n_valid,
+                                void *const *k_out, void *const *v_out, void *hip_stream) {
+  QuantizedArgs a;
+  QuantizedLayers layers;
+  const wkv_status st = plan_rows(shape, n_layers, k_out, v_out, k_codes, k_scales, v_codes, v_scales, &a, &layers);
+  if (st != WKV_OK) return st;
+  if (misaligned(first, 4) || misaligned(n_valid, 4)) return invalid("first and n_valid must be 4-byte aligned");
+  a.n_keep = n_valid; a.first = first;
+  if (a.n_rows == 0) return WKV_OK;
+  return launched(launch_dequantize(a, layers, n_layers, (hipStream_t)hip_stream), "wkv_cache_dequantize");
+}
+
+size_t wkv_decode_quantized_workspace_bytes(const wkv_quantized_shape *shape) {
+  Decode dc;
+  return plan_quantized(shape, &dc) == WKV_OK ? dc.ws_bytes : 0;
+}
+
+wkv_status wkv_decode_step_quantized(const wkv_quantized_shape *shape, const void *q_new, const void *k_new, const void *v_new, void *k_codes,
+                                     void *k_scales, void *v_codes, void *v_scales, int32_t *n_valid, float *out, void *workspace,
+                                     size_t workspace_bytes, void *hip_stream) {
+  Decode dc;
+  wkv_status st = plan_quantized(shape, &dc);
+  if (st != WKV_OK) return st;
+  if (!q_new || !k_new || !v_new || !k_codes || !k_scales || !v_codes || !v_scales || !n_valid || !out)
+    return invalid("q_new / k_new / v_new / k_codes / k_scales / v_codes / v_scales / n_valid / out is NULL");
+  if (misaligned(q_new, 16) || misaligned(k_new, 16) || misaligned(v_new, 16) || misaligned(k_codes, 16) || misaligned(v_codes, 16))
+    return invalid("q_new, k_new, v_new and the codes must be 16-byte aligned");
+  if (misaligned(k_scales, 4) || misaligned(v_scales, 4) || misaligned(n_valid, 4) || misaligned(out, 4))
+    return invalid("the scales, n_valid and out must be 4-byte aligned");
+  st = check_workspace(workspace, workspace_bytes, dc.ws_bytes);
+  if (st != WKV_OK) return st;
+  return launched(launch_decode_quantized(dc.shape, shape->format, q_new, k_new, v_new, k_codes, k_scales, v_codes, v_scales, n_valid, out,
+                                          (float *)workspace, (hipStream_t)hip_stream), "wkv_decode_step_quantized");
+}
+
+size_t wkv_tree_workspace_bytes(const wkv_tree_shape *shape) {
+  TreePlan plan;
+  return plan_tree(shape, &plan) == WKV_OK ? plan.ws_bytes : 0;
+}
+
+wkv_status wkv_decode_tree(const wkv_tree_shape *shape, const void *q_new, const void *k_new, const void *v_new, const int32_t *parent, void *k_cache,
+                           void *v_cache, const int32_t *n_valid, void *out, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  TreePlan plan;
+  wkv_status st = plan_tree(shape, &plan);
+  if (st != WKV_OK) return st;
+  if (!q_new || !k_new || !v_new || !parent || !k_cache || !v_cache || !n_valid || !out)
+    return invalid("q_new / k_new / v_new / parent / k_cache / v_cache / n_valid / out is NULL");
+  if (misaligned(q_new, 16) || misaligned(k_new, 16) || misaligned(v_new, 16) || misaligned(k_cache, 16) || misaligned(v_cache, 16) || misaligned(out, 16))
+    return invalid("q_new, k_new, v_new, the caches and out must be 16-byte aligned");
+  if (misaligned(parent, 4) || misaligned(n_valid, 4)) return invalid("parent and n_valid must be 4-byte aligned");
+  if (out == q_new || out == k_new || out == v_new || out == k_cache || out == v_cache) return invalid("out must not overlap the inputs");
+  st = check_workspace(workspace, workspace_bytes, plan.ws_bytes);
+  if (st != WKV_OK) return st;
+  return launched(launch_tree(plan, q_new, k_new, v_new, parent, k_cache, v_cache, n_valid, out, workspace, (hipStream_t)hip_stream), "wkv_decode_tree");
+}
+
+wkv_status wkv_tree_accept(const wkv_tree_shape *shape, int32_t n_layers, void *const *k_caches, void *const *v_caches, const int32_t *path,
+                           const int32_t *n_accept, int32_t *n_valid, void *hip_stream) {
+  TreePlan plan;
+  const wkv_status st = plan_tree(shape, &plan);
+  if (st != WKV_OK) return st;
+  if (n_layers < 1 || n_layers > WKV_MAX_LAYERS) { set_error("n_layers outside [1, %d]", WKV_MAX_LAYERS); return WKV_ERR_INVALID_ARG; }
+  if (!k_caches || !v_caches || !path || !n_accept || !n_valid) return invalid("k_caches / v_caches / path / n_accept / n_valid is NULL");
+  if (misaligned(path, 4) || misaligned(n_accept, 4) || misaligned(n_valid, 4)) return invalid("path, n_accept and n_valid must be 4-byte aligned");
+  EvictLayers layers;
+  std::memset(&layers, 0, sizeof layers);
+  for (int32_t l = 0; l < n_layers; ++l) {
+    layers.k[l] = k_caches[l]; layers.v[l] = v_caches[l];
+    if (!layers.k[l] || !layers.v[l]) { set_error("cache of layer %d is NULL", l); return WKV_ERR_INVALID_ARG; }
+    if (misaligned(layers.k[l], 16) || misaligned(layers.v[l], 16)) { set_error("caches of layer %d must be 16-byte aligned", l); return WKV_ERR_INVALID_ARG; }
+  }
+  return launched(launch_accept(plan.args, layers, n_layers, path, n_accept, n_valid, (shape->flags & WKV_DECODE_KEEP_COUNT) != 0, (hipStream_t)hip_stream),
+                  "wkv_tree_accept");
+}
+
+}  // extern "C"

@@ -10,8 +10,9 @@ namespace wkv {
 
 namespace {
 
-inline bool misaligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+}  // namespace
 
 wkv_status invalid(const char *what) { set_error("%s", what); return WKV_ERR_INVALID_ARG; }
 wkv_status launched(hipError_t e, const char *what) {
@@ -24,7 +25,6 @@ bool known_dtype(int32_t dtype) {
   set_error("unknown dtype %d", dtype);
   return false;
 }
-constexpr int64_t MAX_STRIDE = (int64_t)1 << 48;      // the address space ends there; products with the bytes of an element and the rows of a tile fit 64 bits
 // Row starts at multiples of 16 bytes, rows of head_dim channels that do not overlap.
 bool good_strides(int32_t dtype, int32_t head_dim, int64_t sb, int64_t sh, int64_t st, const char *what) {
   const int64_t vec = 16 / elem_bytes(dtype);
@@ -42,7 +42,6 @@ wkv_status check_workspace(const void *ws, size_t bytes, size_t needed) {
   if (bytes < needed) { set_error("workspace has %zu bytes, %zu needed", bytes, needed); return WKV_ERR_WORKSPACE; }
   return WKV_OK;
 }
-size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 
 // An angular frequency as turns per token modulo one, in units of 2^-64 turns.  In integers, as 64 divisions of 80-bit floats take 3 us: a double is
 // m * 2^e, and 1 / (2 pi) is TURN * 2^-66 with 64 significant bits.  (A position of 2^31 leaves an error of 2^-33 turns of
@@ -60,8 +59,6 @@ uint64_t turns_of(double inv_freq) {
   else if (shift < 128) turns = (uint64_t)(product >> shift) + (uint64_t)(product >> (shift - 1) & 1);
   return bits >> 63 ? 0 - turns : turns;
 }
-
-}  // namespace
 
 wkv_status plan_rope(const wkv_rope_shape *p, RopeArgs *a) {
   set_error("");

@@ -6,6 +6,17 @@
 
 namespace wkv {
 
+// ---- checks of arguments (with the message of the failure) ----------------------------------------
+constexpr int64_t MAX_STRIDE = (int64_t)1 << 48;      // the address space ends there; products with the bytes of an element and the rows of a tile fit 64 bits
+inline bool misaligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
+inline size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
+wkv_status invalid(const char *what);
+wkv_status launched(hipError_t e, const char *what);
+bool known_dtype(int32_t dtype);
+bool good_strides(int32_t dtype, int32_t head_dim, int64_t sb, int64_t sh, int64_t st, const char *what);
+wkv_status check_workspace(const void *ws, size_t bytes, size_t needed);
+uint64_t turns_of(double inv_freq);
+
 // ---- rotary positions ---------------------------------------------------------------------------
 constexpr int32_t ROPE_PAIRS = 64;        // pairs of channels of a head, at most
 struct RopeTensor {

@@ -23,7 +23,7 @@ PyObject *convert;                                            // callable (o, st
 // may be copied or given another structure), of exactly this type; anything else goes to `convert`, which accepts and
 // refuses what a ctypes call of the same function does.
 struct Kind { PyObject *wrapper, *structure; };
-Kind problem_kind, shape_kind, rope_kind, attention_kind;
+Kind problem_kind, shape_kind, rope_kind, attention_kind, norm_rope_kind, quantized_kind, tree_kind;
 struct Structure {
   Py_buffer view;
   Structure() { view.obj = nullptr; }
@@ -45,6 +45,9 @@ struct Structure {
   const wkv_decode_shape *shape() const { return (const wkv_decode_shape *)view.buf; }
   const wkv_rope_shape *rope() const { return (const wkv_rope_shape *)view.buf; }
   const wkv_attention_shape *attention() const { return (const wkv_attention_shape *)view.buf; }
+  const wkv_norm_rope_shape *norm_rope() const { return (const wkv_norm_rope_shape *)view.buf; }
+  const wkv_quantized_shape *quantized() const { return (const wkv_quantized_shape *)view.buf; }
+  const wkv_tree_shape *tree() const { return (const wkv_tree_shape *)view.buf; }
 };
 
 bool pointer(PyObject *o, void **out) {
@@ -378,12 +381,115 @@ PyObject *cache_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
-// (slow_stream, convert, then each class of structures and the ctypes structure it wraps: Problem, DecodeShape, RopeShape, AttentionShape)
+// (shape, positions, q_weight, k_weight, q_in, q_out, k_in, k_out, stream)
+PyObject *norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  Structure sh;
+  OneDevice at;
+  void *t[7], *st;
+  if (!arity(n, 9) || !sh.fill(a[0], norm_rope_kind)) return nullptr;
+  for (int i = 0; i < 7; ++i) if (!at.pointer(a[1 + i], &t[i])) return nullptr;
+  if (!at.stream(a[8], &st)) return nullptr;
+  return call([&] { return wkv_norm_rope(sh.norm_rope(), (const int32_t *)t[0], t[1], t[2], t[3], t[4], t[5], t[6], st); });
+}
+
+// Sequences of as many tensors each, one a layer.
+template <int N>
+struct LayerPointers {
+  Pointers<WKV_MAX_LAYERS> p[N];
+  bool fill(OneDevice &at, PyObject *const *a) {
+    for (int i = 0; i < N; ++i) if (!at.pointers(a[i], p[i])) return false;
+    for (int i = 1; i < N; ++i)
+      if (p[i].n != p[0].n) { PyErr_SetString(PyExc_ValueError, "as many layers in one sequence as in another"); return false; }
+    return true;
+  }
+  int32_t layers() const { return (int32_t)(p[0].n > WKV_MAX_LAYERS ? WKV_MAX_LAYERS + 1 : p[0].n); }
+};
+
+// (shape, k_layers, v_layers, tok_idx, n_keep, first, k_codes, k_scales, v_codes, v_scales, stream)
+PyObject *cache_quantize(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  Structure sh;
+  OneDevice at;
+  void *t[3], *st;
+  LayerPointers<6> l;
+  if (!arity(n, 11) || !sh.fill(a[0], quantized_kind)) return nullptr;
+  PyObject *const sequences[6] = {a[1], a[2], a[6], a[7], a[8], a[9]};
+  if (!l.fill(at, sequences)) return nullptr;
+  for (int i = 0; i < 3; ++i) if (!at.pointer(a[3 + i], &t[i])) return nullptr;
+  if (!at.stream(a[10], &st)) return nullptr;
+  return call([&] {
+    return wkv_cache_quantize(sh.quantized(), l.layers(), l.p[0].p, l.p[1].p, (const int32_t *)t[0], (const int32_t *)t[1], (const int32_t *)t[2], l.p[2].p,
+                              l.p[3].p, l.p[4].p, l.p[5].p, st);
+  });
+}
+
+// (shape, k_codes, k_scales, v_codes, v_scales, first, n_valid, k_out, v_out, stream)
+PyObject *cache_dequantize(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  Structure sh;
+  OneDevice at;
+  void *t[2], *st;
+  LayerPointers<6> l;
+  if (!arity(n, 10) || !sh.fill(a[0], quantized_kind)) return nullptr;
+  PyObject *const sequences[6] = {a[1], a[2], a[3], a[4], a[7], a[8]};
+  if (!l.fill(at, sequences)) return nullptr;
+  for (int i = 0; i < 2; ++i) if (!at.pointer(a[5 + i], &t[i])) return nullptr;
+  if (!at.stream(a[9], &st)) return nullptr;
+  return call([&] {
+    return wkv_cache_dequantize(sh.quantized(), l.layers(), l.p[0].p, l.p[1].p, l.p[2].p, l.p[3].p, (const int32_t *)t[0], (const int32_t *)t[1], l.p[4].p,
+                                l.p[5].p, st);
+  });
+}
+
+// (shape, q_new, k_new, v_new, k_codes, k_scales, v_codes, v_scales, n_valid, out, workspace, stream)
+PyObject *decode_step_quantized(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  Structure sh;
+  OneDevice at;
+  void *t[9], *ws, *st;
+  size_t bytes;
+  if (!arity(n, 12) || !sh.fill(a[0], quantized_kind)) return nullptr;
+  for (int i = 0; i < 9; ++i) if (!at.pointer(a[1 + i], &t[i])) return nullptr;
+  if (!at.workspace(a[10], &ws, &bytes) || !at.stream(a[11], &st)) return nullptr;
+  return call([&] {
+    return wkv_decode_step_quantized(sh.quantized(), t[0], t[1], t[2], t[3], t[4], t[5], t[6], (int32_t *)t[7], (float *)t[8], ws, bytes, st);
+  });
+}
+
+// (shape, q_new, k_new, v_new, parent, k_cache, v_cache, n_valid, out, workspace, stream)
+PyObject *decode_tree(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  Structure sh;
+  OneDevice at;
+  void *t[8], *ws, *st;
+  size_t bytes;
+  if (!arity(n, 11) || !sh.fill(a[0], tree_kind)) return nullptr;
+  for (int i = 0; i < 8; ++i) if (!at.pointer(a[1 + i], &t[i])) return nullptr;
+  if (!at.workspace(a[9], &ws, &bytes) || !at.stream(a[10], &st)) return nullptr;
+  return call([&] {
+    return wkv_decode_tree(sh.tree(), t[0], t[1], t[2], (const int32_t *)t[3], t[4], t[5], (const int32_t *)t[6], t[7], ws, bytes, st);
+  });
+}
+
+// (shape, k_caches, v_caches, path, n_accept, n_valid, stream)
+PyObject *tree_accept(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  Structure sh;
+  OneDevice at;
+  void *t[3], *st;
+  LayerPointers<2> l;
+  if (!arity(n, 7) || !sh.fill(a[0], tree_kind) || !l.fill(at, a + 1)) return nullptr;
+  for (int i = 0; i < 3; ++i) if (!at.pointer(a[3 + i], &t[i])) return nullptr;
+  if (!at.stream(a[6], &st)) return nullptr;
+  return call([&] {
+    return wkv_tree_accept(sh.tree(), l.layers(), l.p[0].p, l.p[1].p, (const int32_t *)t[0], (const int32_t *)t[1], (int32_t *)t[2], st);
+  });
+}
+
+// (slow_stream, convert, then each class of structures and the ctypes structure it wraps: Problem, DecodeShape, RopeShape, AttentionShape,
+//  NormRopeShape, QuantizedShape, TreeShape)
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  if (!arity(n, 10)) return nullptr;
-  PyObject **to[10] = {&slow_stream, &convert, &problem_kind.wrapper, &problem_kind.structure, &shape_kind.wrapper, &shape_kind.structure,
-                       &rope_kind.wrapper, &rope_kind.structure, &attention_kind.wrapper, &attention_kind.structure};
-  for (int i = 0; i < 10; ++i) {
+  constexpr int N = 16;
+  if (!arity(n, N)) return nullptr;
+  PyObject **to[N] = {&slow_stream, &convert, &problem_kind.wrapper, &problem_kind.structure, &shape_kind.wrapper, &shape_kind.structure,
+                      &rope_kind.wrapper, &rope_kind.structure, &attention_kind.wrapper, &attention_kind.structure, &norm_rope_kind.wrapper,
+                      &norm_rope_kind.structure, &quantized_kind.wrapper, &quantized_kind.structure, &tree_kind.wrapper, &tree_kind.structure};
+  for (int i = 0; i < N; ++i) {
     Py_INCREF(a[i]);
     Py_XSETREF(*to[i], a[i]);
   }
@@ -393,7 +499,8 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(decode_step), FAST(decode_step_static), FAST(score), FAST(window_pool), FAST(topk_windows),
                          FAST(gather_group), FAST(compress_group), FAST(compress_groups),
-                         FAST(rope), FAST(prefill_attention), FAST(decode_step_weighted), FAST(cache_evict),
+                         FAST(rope), FAST(prefill_attention), FAST(decode_step_weighted), FAST(cache_evict), FAST(norm_rope),
+                         FAST(cache_quantize), FAST(cache_dequantize), FAST(decode_step_quantized), FAST(decode_tree), FAST(tree_accept),
                          FAST(bind), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,184 @@
+// Cache rows into 8 and 4 bits and back: bound by memory, which every row crosses once each way.
+//
+// A lane takes eight channels; four lanes share a scale, whose largest magnitude is found by two DPP steps.  The lanes of a row put its scales
+// together, so that they leave in one store.  Rows of all (sequence, KV head) pairs are numbered through, so that a token a sequence fills
+// workgroups as well as a long prompt does.
+#include "wkv_few_bits.h"
+
+namespace wkv {
+
+namespace {
+
+constexpr int QZ_THREADS = 256, AT_ONCE = 4;      // rows of a lane at once
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false); }
+
+// Where row number i of a launch lies: its (sequence, KV head), its own number r, and its place in the cache (-1: none).
+struct RowOf {
+  int bh, r, place;
+  __device__ __forceinline__ RowOf(const QuantizedArgs &a, uint32_t i) {
+    bh = (int)(i / (uint32_t)a.n_rows);
+    r = (int)(i - (uint32_t)bh * (uint32_t)a.n_rows);
+    const int64_t at = (int64_t)(a.first ? a.first[bh] : 0) + r;
+    place = at >= 0 && at < a.capacity ? (int)at : -1;
+  }
+};
+
+template <int DT, int D, int FORMAT>
+__global__ __launch_bounds__(QZ_THREADS) void quantize_kernel(QuantizedArgs a, QuantizedLayers layers) {
+  constexpr int LPR = D / 8, UNITS = QZ_THREADS / LPR, PIECES = DT == DT_F32 ? 2 : 1, SB = D / SCALE_GROUP;
+  const int layer = blockIdx.z >> 1, is_v = blockIdx.z & 1;
+  const char *plain = (const char *)layers.plain[is_v][layer];
+  char *codes = (char *)layers.codes[is_v][layer], *scales = (char *)layers.scales[is_v][layer];
+  const int lane = threadIdx.x % LPR, unit = threadIdx.x / LPR;
+  const int64_t total = (int64_t)a.heads * a.n_rows, i0 = (int64_t)blockIdx.x * (UNITS * AT_ONCE) + unit;
+
+  uint4 x[AT_ONCE][PIECES];
+  int bh[AT_ONCE], place[AT_ONCE];
+#pragma unroll
+  for (int u = 0; u < AT_ONCE; ++u) {
+    const int64_t i = i0 + u * UNITS;
+    place[u] = -1;
+    if (i >= total) continue;
+    const RowOf row(a, (uint32_t)i);
+    bh[u] = row.bh;
+    place[u] = a.n_keep && row.r >= a.n_keep[row.bh] ? -1 : row.place;
+    int from = row.r;
+    if (a.tok_idx) {
+      from = a.tok_idx[i];
+      if (from < 0 || from >= a.row_capacity) place[u] = -1;
+    }
+    if (place[u] < 0) continue;
+    const int b = divide((uint32_t)row.bh, a.kv_magic), h = row.bh - b * a.Hkv;
+    const char *in = plain + (b * a.r_sb + h * a.r_sh + from * a.r_st) + lane * (16 * PIECES);
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) x[u][k] = *(const uint4 *)(in + k * 16);
+  }
+#pragma unroll
+  for (int u = 0; u < AT_ONCE; ++u) {
+    if (place[u] < 0) continue;                  // (the same in all lanes of a row)
+    float f[8];
+    widen<DT>(x[u][0], f);
+    if constexpr (PIECES == 2) widen<DT>(x[u][1], f + 4);
+    uint32_t largest = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) largest = max(largest, __float_as_uint(f[e]) & 0x7fffffffu);
+    largest = max(largest, dpp<0xB1>(largest));                  // quad_perm [1,0,3,2]
+    largest = max(largest, dpp<0x4E>(largest));                  // quad_perm [2,3,0,1]
+    const uint32_t byte = (uint32_t)scale_byte<FORMAT>(largest);
+    const float scale = scale_of(byte);
+    const int b = divide((uint32_t)bh[u], a.kv_magic), h = bh[u] - b * a.Hkv;
+    char *to = codes + (b * a.c_sb + h * a.c_sh + place[u] * a.c_st);
+    if constexpr (FORMAT == E4M3) {
+      uint32_t lo = to_codes<FORMAT, 1>(to_codes<FORMAT, 0>(0, f[0], f[1], scale), f[2], f[3], scale);
+      uint32_t hi = to_codes<FORMAT, 1>(to_codes<FORMAT, 0>(0, f[4], f[5], scale), f[6], f[7], scale);
+      if (byte == NO_SCALE) lo = hi = 0;
+      *(u32x2 *)(to + lane * 8) = (u32x2){lo, hi};
+    } else {
+      uint32_t w = to_codes<FORMAT, 1>(to_codes<FORMAT, 0>(0, f[0], f[1], scale), f[2], f[3], scale);
+      w = to_codes<FORMAT, 3>(to_codes<FORMAT, 2>(w, f[4], f[5], scale), f[6], f[7], scale);
+      if (byte == NO_SCALE) w = 0;
+      *(uint32_t *)(to + lane * 4) = w;
+    }
+    uint32_t all = byte << (lane / 4 * 8);
+    char *sc = scales + ((int64_t)bh[u] * a.capacity + place[u]) * SB;
+    if constexpr (D == 128) {
+      all |= dpp<0x124>(all);                                    // row_ror:4
+      all |= dpp<0x128>(all);                                    // row_ror:8
+      if (lane == 0) *(uint32_t *)sc = all;
+    } else {
+      all |= dpp<0x141>(all);                                    // row_half_mirror
+      if (lane == 0) *(uint16_t *)sc = (uint16_t)all;
+    }
+  }
+}
+
+template <int DT, int D, int FORMAT>
+__global__ __launch_bounds__(QZ_THREADS) void dequantize_kernel(QuantizedArgs a, QuantizedLayers layers) {
+  constexpr int LPR = D / 8, UNITS = QZ_THREADS / LPR, SB = D / SCALE_GROUP, WORDS = FORMAT == E4M3 ? 2 : 1;
+  const int layer = blockIdx.z >> 1, is_v = blockIdx.z & 1;
+  char *plain = (char *)layers.plain[is_v][layer];
+  const char *codes = (const char *)layers.codes[is_v][layer];
+  const uint8_t *scales = (const uint8_t *)layers.scales[is_v][layer];
+  const int lane = threadIdx.x % LPR, unit = threadIdx.x / LPR;
+  const int64_t total = (int64_t)a.heads * a.n_rows, i0 = (int64_t)blockIdx.x * (UNITS * AT_ONCE) + unit;
+
+  uint32_t x[AT_ONCE][WORDS], byte[AT_ONCE];
+  char *to[AT_ONCE];
+#pragma unroll
+  for (int u = 0; u < AT_ONCE; ++u) {
+    const int64_t i = i0 + u * UNITS;
+    to[u] = nullptr;
+    if (i >= total) continue;
+    const RowOf row(a, (uint32_t)i);
+    if (row.place < 0 || (a.n_keep && row.place >= a.n_keep[row.bh])) continue;
+    const int b = divide((uint32_t)row.bh, a.kv_magic), h = row.bh - b * a.Hkv;
+    const char *in = codes + (b * a.c_sb + h * a.c_sh + row.place * a.c_st) + lane * (WORDS * 4);
+    if constexpr (WORDS == 2) { const u32x2 w = *(const u32x2 *)in; x[u][0] = w[0]; x[u][1] = w[1]; }
+    else x[u][0] = *(const uint32_t *)in;
+    byte[u] = scales[((int64_t)row.bh * a.capacity + row.place) * SB + lane / 4];
+    to[u] = plain + (b * a.r_sb + h * a.r_sh + row.r * a.r_st) + lane * (DT == DT_F32 ? 32 : 16);
+  }
+#pragma unroll
+  for (int u = 0; u < AT_ONCE; ++u) {
+    if (!to[u]) continue;
+    const float scale = scale_of(byte[u]);
+    if constexpr (DT == DT_BF16) {
+      u32x4 y;
+      if constexpr (FORMAT == E4M3)
+        y = (u32x4){bf16_pair<FORMAT, 0>(x[u][0], scale), bf16_pair<FORMAT, 1>(x[u][0], scale), bf16_pair<FORMAT, 0>(x[u][1], scale), bf16_pair<FORMAT, 1>(x[u][1], scale)};
+      else
+        y = (u32x4){bf16_pair<FORMAT, 0>(x[u][0], scale), bf16_pair<FORMAT, 1>(x[u][0], scale), bf16_pair<FORMAT, 2>(x[u][0], scale), bf16_pair<FORMAT, 3>(x[u][0], scale)};
+      *(u32x4 *)to[u] = y;
+    } else {
+      float2 f[4];
+      f[0] = float_pair<FORMAT, 0>(x[u][0], scale);
+      f[1] = float_pair<FORMAT, 1>(x[u][0], scale);
+      f[2] = float_pair<FORMAT, FORMAT == E4M3 ? 0 : 2>(x[u][WORDS - 1], scale);
+      f[3] = float_pair<FORMAT, FORMAT == E4M3 ? 1 : 3>(x[u][WORDS - 1], scale);
+      if constexpr (DT == DT_F32) {
+        ((float4 *)to[u])[0] = make_float4(f[0].x, f[0].y, f[1].x, f[1].y);
+        ((float4 *)to[u])[1] = make_float4(f[2].x, f[2].y, f[3].x, f[3].y);
+      } else {
+        // past the largest number of the type: that one (a value may have been rounded up to 2^16); NaN stays
+        auto half = [](float v) { return (_Float16)(v > 65504.0f ? 65504.0f : v < -65504.0f ? -65504.0f : v); };
+        typedef _Float16 f16x8v __attribute__((ext_vector_type(8)));
+        *(f16x8v *)to[u] = (f16x8v){half(f[0].x), half(f[0].y), half(f[1].x), half(f[1].y), half(f[2].x), half(f[2].y), half(f[3].x), half(f[3].y)};
+      }
+    }
+  }
+}
+
+template <int DT, int D, int FORMAT>
+hipError_t launch_as(bool back, const QuantizedArgs &a, const QuantizedLayers &layers, int32_t n_layers, hipStream_t stream) {
+  constexpr int ROWS = QZ_THREADS / (D / 8) * AT_ONCE;
+  const int64_t total = (int64_t)a.heads * a.n_rows;
+  const dim3 grid((uint32_t)((total + ROWS - 1) / ROWS), 1, (uint32_t)n_layers * 2);
+  if (back) hipLaunchKernelGGL((dequantize_kernel<DT, D, FORMAT>), grid, dim3(QZ_THREADS), 0, stream, a, layers);
+  else hipLaunchKernelGGL((quantize_kernel<DT, D, FORMAT>), grid, dim3(QZ_THREADS), 0, stream, a, layers);
+  return hipGetLastError();
+}
+template <int DT>
+hipError_t launch_type(bool back, const QuantizedArgs &a, const QuantizedLayers &layers, int32_t n_layers, hipStream_t stream) {
+  if (a.format == E4M3) return a.d == 128 ? launch_as<DT, 128, E4M3>(back, a, layers, n_layers, stream) : launch_as<DT, 64, E4M3>(back, a, layers, n_layers, stream);
+  return a.d == 128 ? launch_as<DT, 128, E2M1>(back, a, layers, n_layers, stream) : launch_as<DT, 64, E2M1>(back, a, layers, n_layers, stream);
+}
+hipError_t launch_rows(bool back, const QuantizedArgs &a, const QuantizedLayers &layers, int32_t n_layers, hipStream_t stream) {
+  if (a.dtype == WKV_BF16) return launch_type<DT_BF16>(back, a, layers, n_layers, stream);
+  if (a.dtype == WKV_F16) return launch_type<DT_F16>(back, a, layers, n_layers, stream);
+  return launch_type<DT_F32>(back, a, layers, n_layers, stream);
+}
+
+}  // namespace
+
+hipError_t launch_quantize(const QuantizedArgs &a, const QuantizedLayers &layers, int32_t n_layers, hipStream_t stream) {
+  return launch_rows(false, a, layers, n_layers, stream);
+}
+hipError_t launch_dequantize(const QuantizedArgs &a, const QuantizedLayers &layers, int32_t n_layers, hipStream_t stream) {
+  return launch_rows(true, a, layers, n_layers, stream);
+}
+
+}  // namespace wkv
