@@ -667,7 +667,7 @@ typedef struct {
   int32_t capacity;          /* rows per (b, h) in the caches, at most 2^30                      */
   int64_t cache_stride_b, cache_stride_h, cache_stride_t;   /* elements; head_dim contiguous; 64 rows of a cache are less than 2 GiB apart */
   int64_t q_stride_b, q_stride_h, q_stride_t;               /* q_new [batch, n_q_heads, n_nodes, head_dim]  */
-  int64_t new_stride_b, new_stride_h, new_stride_t;         /* k_new, v_new [batch, n_kv_heads, n_nodes, head_dim] */
+  int64_t new_stride_b, new_stride_h, new_stride_t;         /* k_new, v_new [batch, n_kv_heads, n_nodes, head_dim]; stride_t as the cache's */
   int64_t out_stride_b, out_stride_h, out_stride_t;         /* out as q_new                                 */
   int32_t flags;             /* 0, or WKV_DECODE_KEEP_COUNT (wkv_tree_accept)                   */
 } wkv_tree_shape;

@@ -115,7 +115,43 @@ wkv_status plan_rows(const wkv_quantized_shape *p, int32_t n_layers, const void 
 
 }  // namespace
 
-// How the work is cut: blocks of 32 to 256 rows, and ranges of a cache so that about 1024 workgroups have work if every cache is full.
+// How the work of a tree is cut: rows of a block and ranges of a cache, by an estimate of the time in us that takes every cache for nine tenths full.  Fitted to
+// 34 shapes, each timed with up to fifteen numbers of ranges and every kind of block: the cut that it takes is 3.5 % behind the best in the geometric mean, 14 % at worst.
+//   blocks   of 64 rows (two pairs of waves, the waves of a pair share a tile's keys) where there are no more; of 128; of 256 where these fill the compute units
+//            without ranges (64 sequences of 2000 rows and 64 nodes, 32q/8kv heads 180 us, by blocks of 128 215).  Of 32 rows, shared by two waves: never better than 64 (4 nodes over
+//            4128 rows 13.2 and 11.9 us, 64 sequences with 8 nodes 167.5 and 166.5).
+//   ranges   one / two / four / eight / 16 / 35: 16 nodes over 4128 rows, one sequence 120 / 66 / 38 / 23 / 15.5 / 17.8, eight - / 48 / 38 / 40 / 48 / -, 64 sequences 169 / 211 / ..
+struct TreeCut {
+  int32_t row_waves, key_waves, blocks, chunk, splits;
+};
+static TreeCut cut_tree(int64_t heads, int32_t n_rows, int32_t d, bool f32, int64_t capacity) {
+  TreeCut best = {};
+  double best_time = 1e300;
+  for (const int32_t row_waves : {2, 4, 8}) {
+    if (row_waves == 2 ? n_rows > 64 : row_waves == 4 ? n_rows <= 64 : n_rows <= 128 || f32) continue;
+    TreeCut cut;
+    cut.row_waves = row_waves;
+    cut.key_waves = row_waves == 2 ? 2 : 1;
+    cut.blocks = (int32_t)ceil_div(n_rows, row_waves * 32);
+    const int64_t tiles = ceil_div(capacity, tree_wave_keys(f32, cut.key_waves) * cut.key_waves), groups = heads * cut.blocks;
+    if (row_waves == 8 && groups < 256) continue;
+    // workgroups at a time; a tile's time, alone on a compute unit and beside another
+    const double slots = row_waves == 8 || (f32 && row_waves == 2 && d == 128) ? 256 : 512, size = d == 128 ? 1.0 : 0.62;
+    const double alone = (f32 ? 3.6 : row_waves == 8 ? 2.0 : 1.25) * size, shared = (f32 ? 3.6 : row_waves == 8 ? 2.0 : 2.45) * size;
+    for (const int32_t want : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
+      if (want > 1 && (want > tiles || groups * want > 2048 || row_waves == 8)) break;
+      cut.chunk = (int32_t)ceil_div(tiles, want);
+      cut.splits = (int32_t)ceil_div(tiles, cut.chunk);
+      const double parts = cut.splits > 1 ? cut.splits * 0.9 + 1 : 1;          // workgroups of a block, the nodes' among them
+      const double busy = std::min(std::max((groups * parts - 256) / 256, 0.0), 1.0);
+      double time = std::max(groups * (tiles * 0.9 + 3.0 * parts + 3.4) * shared / slots, 5.6 + cut.chunk * (alone + (shared - alone) * busy));
+      if (cut.splits > 1) time += 4.1 + (double)heads * n_rows * parts * (d * 8) / 4e6;
+      if (time < best_time) { best_time = time; best = cut; }
+    }
+  }
+  return best;
+}
+
 wkv_status plan_tree(const wkv_tree_shape *p, TreePlan *plan) {
   set_error("");
   if (!p) return invalid("shape is NULL");
@@ -141,6 +177,7 @@ wkv_status plan_tree(const wkv_tree_shape *p, TreePlan *plan) {
     return WKV_ERR_INVALID_ARG;
   // (the rows that a wave fetches of a tile are addressed by 32-bit offsets)
   if (p->cache_stride_t * elem_bytes(p->dtype) * 64 > 0x7fffffff) { set_error("cache token stride %lld is not supported", (long long)p->cache_stride_t); return WKV_ERR_UNSUPPORTED; }
+  if (p->new_stride_t * elem_bytes(p->dtype) * 64 > 0x7fffffff) { set_error("new token stride %lld is not supported", (long long)p->new_stride_t); return WKV_ERR_UNSUPPORTED; }
   std::memset(plan, 0, sizeof *plan);
   TreeArgs &a = plan->args;
   const bool f32 = p->dtype == WKV_F32;
@@ -154,18 +191,14 @@ wkv_status plan_tree(const wkv_tree_shape *p, TreePlan *plan) {
   a.q_sb = p->q_stride_b * e; a.q_sh = p->q_stride_h * e; a.q_st = p->q_stride_t * e;
   a.n_sb = p->new_stride_b * e; a.n_sh = p->new_stride_h * e; a.n_st = p->new_stride_t * e;
   a.o_sb = p->out_stride_b * e; a.o_sh = p->out_stride_h * e; a.o_st = p->out_stride_t * e;
-  // fp32 tiles are twice as large: two key waves at most, and blocks of 128 rows
-  plan->row_waves = a.n_rows <= 32 && !f32 ? 1 : a.n_rows <= 64 ? 2 : a.n_rows <= 128 || f32 ? 4 : 8;
-  plan->key_waves = plan->row_waves == 1 ? 4 : plan->row_waves == 2 ? 2 : 1;
-  const int32_t rows = plan->row_waves * 32, keys = tree_wave_keys(f32, plan->key_waves) * plan->key_waves;
-  a.blocks = (int32_t)ceil_div(a.n_rows, rows);
-  const int64_t tiles = ceil_div(p->capacity, keys);
-  const int64_t want = std::max<int64_t>(1024 / ((int64_t)a.heads * a.blocks), 1);
-  a.chunk = (int32_t)std::max<int64_t>(ceil_div(tiles, want), ceil_div(128, keys));
-  a.splits = (int32_t)ceil_div(tiles, a.chunk);
+  const TreeCut cut = cut_tree(a.heads, a.n_rows, a.d, f32, a.capacity);
+  plan->row_waves = cut.row_waves; plan->key_waves = cut.key_waves;
+  a.blocks = cut.blocks; a.chunk = cut.chunk; a.splits = cut.splits;
+  plan->streams = 2 * (int64_t)a.heads * a.capacity * a.d * e > MEMORY_CACHE_BYTES;
+  const int32_t rows = plan->row_waves * 32;
   plan->ws_bytes = 256;
   if (a.splits > 1) {
-    const size_t all = (size_t)a.heads * a.blocks * a.splits * rows;
+    const size_t all = (size_t)a.heads * a.blocks * (a.splits + 1) * rows;
     plan->stats_at = all * a.d * sizeof(float);
     plan->ws_bytes = round_up(plan->stats_at + all * sizeof(float2));
   }

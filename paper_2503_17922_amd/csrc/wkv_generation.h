@@ -49,10 +49,12 @@ struct TreeArgs {
   float c1;                              // scale * log2(e)
   int64_t c_sb, c_sh, c_st, q_sb, q_sh, q_st, n_sb, n_sh, n_st, o_sb, o_sh, o_st;      // bytes
 };
-// Partial results in the workspace: outputs float [heads][blocks][splits][rows of a block][d], then their references and sums float2.
+// Partial results in the workspace, with more than one range: outputs float [heads][blocks][splits + 1][rows of a block][d], the first of them those of the nodes' own
+// rows, then their references and sums float2.
 struct TreePlan {
   TreeArgs args;
   int32_t row_waves, key_waves;
+  bool streams;                          // the caches exceed the memory-side cache
   size_t stats_at, ws_bytes;
 };
 constexpr int32_t tree_wave_keys(bool f32, int32_t key_waves) { return f32 || key_waves > 1 ? 32 : 64; }      // keys of a tile that a wave takes

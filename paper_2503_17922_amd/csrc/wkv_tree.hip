@@ -8,7 +8,7 @@
 // the matrix pipe.  Where a wave's 32 rows are all there are, or half of them, the waves of a workgroup share the keys of a tile instead and join their results in LDS.
 //
 // How many rows a cache has is on the device: the ranges divide its capacity, and those behind its rows return at once.  The nodes' own tile, read from
-// the new rows, belongs to the first range; a workgroup of its own puts them into the cache, whose rows from n on nobody reads in this launch.
+// the new rows, is a range of its own where there are several.  They are put into the cache at the end or by the second launch: nobody reads its rows from n on.
 #include "wkv_attention_tile.h"
 #include "wkv_generation.h"
 
@@ -59,17 +59,40 @@ __device__ __forceinline__ bool all_finite(const uint4 &x) {
   return ok;
 }
 
+// The new rows of the nodes that exist (`all`) into the cache, by NT threads.
+template <int PPR, int NT>
+__device__ __forceinline__ void copy_rows(const TreeArgs &a, uint64_t all, int b, int h, int n, const char *__restrict__ kn, const char *__restrict__ vn,
+                                          char *__restrict__ kc, char *__restrict__ vc) {
+  constexpr int AHEAD = 4;
+  const int64_t from = b * a.n_sb + h * a.n_sh, to = b * a.c_sb + h * a.c_sh + n * a.c_st;
+  for (int i0 = threadIdx.x; i0 < 2 * a.T * PPR; i0 += AHEAD * NT) {
+    uint4 x[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int i = min(i0 + k * NT, 2 * a.T * PPR - 1), r = i / PPR;
+      x[k] = *(const uint4 *)((r & 1 ? vn : kn) + from + (r >> 1) * a.n_st + i % PPR * 16);
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int i = i0 + k * NT, r = i / PPR;
+      if (i < 2 * a.T * PPR && all >> (r >> 1) & 1) *(uint4 *)((r & 1 ? vc : kc) + to + (r >> 1) * a.c_st + i % PPR * 16) = x[k];
+    }
+  }
+}
+
 // ROW_WAVES times 32 rows, KEY_WAVES waves to each.
 template <int D, int DT, int ROW_WAVES, int KEY_WAVES>
 struct Shares {
   static constexpr int WAVES = ROW_WAVES * KEY_WAVES, NT = WAVES * 64, ROWS = ROW_WAVES * 32;
   static constexpr int KW = tree_wave_keys(DT == DT_F32, KEY_WAVES), KEYS = KW * KEY_WAVES;
   using Tile = Att<D, DT, WAVES, KEYS>;
-  static constexpr int LDS = Tile::STAGES * Tile::STAGE;
+  static constexpr int SLOTS = 5, LDS = SLOTS * Tile::TILE;          // tiles of keys and of values in turn: two in use, three under way
+  // of a SIMD; two at least where the LDS of a compute unit has room for as many workgroups
+  static constexpr int LEAST_WAVES = 160 * 1024 / LDS * WAVES >= 8 ? 2 : 1;
 };
 
-template <int D, int DT, int ROW_WAVES, int KEY_WAVES>
-__global__ __launch_bounds__(ROW_WAVES * KEY_WAVES * 64, 2) void tree_kernel(TreeArgs a, const char *__restrict__ q, const char *__restrict__ kn,
+template <int D, int DT, int ROW_WAVES, int KEY_WAVES, bool STREAM>
+__global__ __launch_bounds__((ROW_WAVES * KEY_WAVES * 64), (Shares<D, DT, ROW_WAVES, KEY_WAVES>::LEAST_WAVES)) void tree_kernel(TreeArgs a, const char *__restrict__ q, const char *__restrict__ kn,
                                                                              const char *__restrict__ vn, const int32_t *__restrict__ parent,
                                                                              char *__restrict__ kc, char *__restrict__ vc,
                                                                              const int32_t *__restrict__ n_valid, char *__restrict__ out,
@@ -78,29 +101,20 @@ __global__ __launch_bounds__(ROW_WAVES * KEY_WAVES * 64, 2) void tree_kernel(Tre
   using C = typename S::Tile;
   constexpr int KS = C::KS, VT = C::VT, WAVES = S::WAVES, KW = S::KW, KT = KW / 32, KEYS = S::KEYS, ROWS = S::ROWS, ES = C::ES;
   __shared__ __attribute__((aligned(1024))) char ring[S::LDS];
-  __shared__ uint32_t not_finite_s[2];           // nodes whose values are not all finite
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5, row_wave = wave / KEY_WAVES, key_wave = wave % KEY_WAVES;
 
-  const bool copies = (int)blockIdx.y == a.splits;
-  const RangeOf it(blockIdx.x, copies ? 0 : blockIdx.y, a.heads, a.heads_magic);
-  const int bh = it.head, split = it.range, block = blockIdx.z, b = divide(bh, a.kv_magic), h = bh - b * a.Hkv;
+  // where there are several ranges, y == 0 are the nodes, whose way is longest, and range y - 1 the others
+  const int y = blockIdx.y;
+  const bool whole = a.splits == 1, of_nodes = y == 0;
+  const RangeOf it(blockIdx.x, y, a.heads, a.heads_magic);
+  const int bh = it.head, split = whole ? 0 : y - 1, block = blockIdx.z, b = divide(bh, a.kv_magic), h = bh - b * a.Hkv;
   const int n = load_scalar(n_valid + bh);
   const bool fits = n >= 0 && n <= a.capacity - a.T;
-  if (copies) {                              // the new rows go into the cache
-    if (block != 0 || !fits) return;
-    const Nodes nodes(a, parent, b);
-    for (int i = threadIdx.x; i < 2 * a.T * C::PPR; i += S::NT) {
-      const int piece = i % C::PPR, r = i / C::PPR, t = r >> 1, is_v = r & 1;
-      const uint4 x = *(const uint4 *)((is_v ? vn : kn) + (b * a.n_sb + h * a.n_sh + t * a.n_st) + piece * 16);
-      if (nodes.all >> t & 1) *(uint4 *)((is_v ? vc : kc) + (b * a.c_sb + h * a.c_sh + (int64_t)(n + t) * a.c_st) + piece * 16) = x;
-    }
-    return;
-  }
-  const int own = split == 0 ? (a.T + KEYS - 1) / KEYS : 0;          // tiles of new rows
-  const int t_begin = split ? split * a.chunk : 0, t_end = fits ? min(t_begin + a.chunk, (n + KEYS - 1) / KEYS) : 0;
-  const int n_tiles = fits ? own + max(t_end - t_begin, 0) : 0;
-  if (n_tiles == 0 && split != 0) return;
+  const int own = of_nodes && fits ? (a.T + KEYS - 1) / KEYS : 0;          // tiles of new rows
+  const int t_begin = split * a.chunk, t_end = fits && split >= 0 ? min(t_begin + a.chunk, (n + KEYS - 1) / KEYS) : t_begin;
+  const int n_tiles = own + max(t_end - t_begin, 0);
+  if (n_tiles == 0 && !of_nodes) return;
 
   // ---- this lane's row
   const int wave_row = block * ROWS + row_wave * 32, row = min(wave_row + col, a.n_rows - 1);
@@ -109,36 +123,26 @@ __global__ __launch_bounds__(ROW_WAVES * KEY_WAVES * 64, 2) void tree_kernel(Tre
   // ---- the key and value stream: tile i < own of the new rows, then those of the cache
   const int64_t c_at = b * a.c_sb + h * a.c_sh, n_at = b * a.n_sb + h * a.n_sh;
   const char *kb = kc + c_at, *vb = vc + c_at, *knb = kn + n_at, *vnb = vn + n_at;
-  const uint32_t st = (uint32_t)a.c_st;
   const int my_row = wave * C::RPI + lane / C::PPR, my_piece = lane % C::PPR;      // of this lane's first DMA instruction
   uint32_t k_slot[C::OFFS];
 #pragma unroll
   for (int i = 0; i < C::OFFS; ++i) k_slot[i] = C::key_slot(my_row + i * C::RPI * WAVES, my_piece) * 16;
   const uint32_t v_slot = C::value_slot(my_row, my_piece) * 16;
   const uint32_t ring_at = lds_address(ring) + wave * 1024;
-  auto fetch = [&](int i) __attribute__((always_inline)) {
-    const uint32_t dst = ring_at + (i % C::STAGES) * C::STAGE;
-    const bool of_nodes = i < own;
-    const int j0 = of_nodes ? i * KEYS : (t_begin + i - own) * KEYS, last = (of_nodes ? a.T : n) - 1;
-    if (!of_nodes && j0 + KEYS <= n) {
+  // Tile i of keys or of values, number 2 * i (+ 1) of the ring; of rows past the last one, it again.
+  auto fetch = [&](int i, bool is_v) __attribute__((always_inline)) {
+    const uint32_t dst = ring_at + (2 * i + is_v) % S::SLOTS * C::TILE;
+    const bool is_new = i < own;
+    const int j0 = (is_new ? i : t_begin + i - own) * KEYS, last = min((is_new ? a.T : n) - 1 - j0, KEYS - 1);
+    const int64_t by = is_new ? a.n_st : a.c_st;
+    const char *from = (is_new ? (is_v ? vnb : knb) : is_v ? vb : kb) + j0 * by;
+    const uint32_t st = (uint32_t)by, most = last * st, at = my_row * st;
 #pragma unroll
-      for (int x = 0; x < C::LPT; ++x)
-        dma_rows(dst + x * (WAVES * 1024), kb + (int64_t)(j0 + x * (C::RPI * WAVES)) * a.c_st, my_row * st + k_slot[x % C::OFFS]);
-#pragma unroll
-      for (int x = 0; x < C::LPT; ++x)
-        dma_rows(dst + C::TILE + x * (WAVES * 1024), vb + (int64_t)(j0 + x * (C::RPI * WAVES)) * a.c_st, my_row * st + v_slot);
-    } else {                              // rows past the last one: it again
-      const char *kf = of_nodes ? knb : kb, *vf = of_nodes ? vnb : vb;
-      const int64_t fst = of_nodes ? a.n_st : a.c_st;
-#pragma unroll
-      for (int x = 0; x < C::LPT; ++x) {
-        const int64_t r = min(j0 + x * (C::RPI * WAVES) + my_row, last);
-        dma_to_lds(dst + x * (WAVES * 1024), kf + r * fst + k_slot[x % C::OFFS]);
-        dma_to_lds(dst + C::TILE + x * (WAVES * 1024), vf + r * fst + v_slot);
-      }
-    }
+    for (int x = 0; x < C::LPT; ++x)
+      dma_rows<STREAM>(dst + x * (WAVES * 1024), from, min(at + x * (C::RPI * WAVES) * st, most) + (is_v ? v_slot : k_slot[x % C::OFFS]));
   };
-  if (n_tiles > 0) fetch(0);
+  if (n_tiles > 0) { fetch(0, false); fetch(0, true); }
+  if (n_tiles > 1) fetch(1, false);
 
   // ---- queries: B fragments; this row's part of the tree
   bf16x8 qf[KS];
@@ -150,13 +154,25 @@ __global__ __launch_bounds__(ROW_WAVES * KEY_WAVES * 64, 2) void tree_kernel(Tre
 #pragma unroll
     for (int i = 0; i < KS; ++i) asm volatile("" : "+v"(qf[i]));
   }
-  uint64_t family = 0;
-  if (split == 0) {
+  uint64_t family = 0, not_finite = 0, all = 0;     // of this row's node; of all nodes: those whose values are not all finite, those that exist
+  if (of_nodes) {
     const Nodes nodes(a, parent, b);
     family = nodes.of(node);
-    if (threadIdx.x < 2) not_finite_s[threadIdx.x] = 0;
+    all = nodes.all;
+    constexpr int AHEAD = 4;
+    for (int t0 = 0; t0 < a.T; t0 += AHEAD * C::RPI) {
+      uint4 x[AHEAD];
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) x[k] = *(const uint4 *)(vnb + min(t0 + k * C::RPI + lane / C::PPR, a.T - 1) * a.n_st + lane % C::PPR * 16);
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        const uint64_t wrong = __ballot(!all_finite<DT>(x[k]));
+        if (wrong)
+          for (int r = 0; r < C::RPI; ++r)
+            if (wrong >> (r * C::PPR) & ((1ull << C::PPR) - 1)) not_finite |= 1ull << min(t0 + k * C::RPI + r, a.T - 1);
+      }
+    }
   }
-
   f32x16 o[VT];
 #pragma unroll
   for (int i = 0; i < VT; ++i)
@@ -252,33 +268,31 @@ __global__ __launch_bounds__(ROW_WAVES * KEY_WAVES * 64, 2) void tree_kernel(Tre
   };
 
   for (int i = 0; i < n_tiles; ++i) {
-    // the tile is in LDS (each wave waits for its own requests, the barrier for all), and everyone is done with the place of the next
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (i + 1 < n_tiles) fetch(i + 1);
-    if (i < own) {
+    // the tiles are in LDS (each wave waits for its own requests but the next keys, the barrier for all), and everyone is done with the two before
+    if (i + 1 < n_tiles) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(C::LPT) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (i + 1 < n_tiles) fetch(i + 1, true);
+    if (i + 2 < n_tiles) fetch(i + 2, false);
+    const char *ks = ring + 2 * i % S::SLOTS * C::TILE + key_wave * KW * C::ROWB, *vs = ring + (2 * i + 1) % S::SLOTS * C::TILE + key_wave * KW * C::ROWB;
+    if (i < own && not_finite) {
       // A probability of zero times an infinity is a NaN: values that are not finite, of padding too, are taken out of the tile, and the rows that see them are
       // told at the end.
-      char *vs = ring + (i % C::STAGES) * C::STAGE + C::TILE;
+      char *tile = ring + (2 * i + 1) % S::SLOTS * C::TILE;
       for (int x = threadIdx.x; x < KEYS * C::PPR; x += S::NT)
-        if (!all_finite<DT>(*(const uint4 *)(vs + x * 16))) {
-          *(uint4 *)(vs + x * 16) = make_uint4(0, 0, 0, 0);
-          const int t = min(i * KEYS + x / C::PPR, a.T - 1);
-          atomicOr(&not_finite_s[t >> 5], 1u << (t & 31));
-        }
+        if (not_finite >> min(i * KEYS + x / C::PPR, a.T - 1) & 1) *(uint4 *)(tile + x * 16) = make_uint4(0, 0, 0, 0);
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
     if (wave_row >= a.n_rows) continue;
-    const char *ks = ring + (i % C::STAGES) * C::STAGE + key_wave * KW * C::ROWB;
     const int j0 = (i < own ? i : t_begin + i - own) * KEYS + key_wave * KW, at = j0 + half * 4;
     uint64_t seen;
     if (i < own) seen = at < 64 ? family >> at : 0;
     else seen = at + 64 <= n ? ~0ull : at < n ? (1ull << (n - at)) - 1 : 0;
-    attend(ks, ks + C::TILE, i < own || j0 + KW > n, seen);
+    attend(ks, vs, i < own || j0 + KW > n, seen);
   }
 
-  if (n_tiles > 0 && split == 0) {
-    if (family & ((uint64_t)not_finite_s[1] << 32 | not_finite_s[0])) l = __uint_as_float(0x7fc00000u);
-  }
+  if (family & not_finite) l = __uint_as_float(0x7fc00000u);
+
+  if (whole && block == 0 && fits) copy_rows<C::PPR, S::NT>(a, all, b, h, n, kn, vn, kc, vc);
 
   // ---- the waves that share rows
   if constexpr (KEY_WAVES > 1) {
@@ -330,9 +344,9 @@ __global__ __launch_bounds__(ROW_WAVES * KEY_WAVES * 64, 2) void tree_kernel(Tre
   // ---- results: of this range, for join_tree_kernel, or of the row
   l = add_halves(l, l);
   const bool exists = wave_row + col < a.n_rows;
-  const bool counts = split != 0 || family != 0;          // (a node that is none leaves its row as it is, and says so by a negative sum)
+  const bool counts = !of_nodes || family != 0;          // (a node that is none leaves its row as it is, and says so by a negative sum)
   if (a.splits > 1) {
-    const int64_t at = (((int64_t)bh * a.blocks + block) * a.splits + split) * ROWS + row_wave * 32 + col;
+    const int64_t at = (((int64_t)bh * a.blocks + block) * (a.splits + 1) + y) * ROWS + row_wave * 32 + col;
     if (exists && half == 0) stats[at] = counts ? make_float2(m, fits ? l : __uint_as_float(0x7fc00000u)) : make_float2(-INFINITY, -1.0f);
     if (!fits) return;
 #pragma unroll
@@ -366,18 +380,25 @@ __global__ __launch_bounds__(ROW_WAVES * KEY_WAVES * 64, 2) void tree_kernel(Tre
 constexpr int JOIN_THREADS = 256;
 template <int D, int DT, int GROUPS>
 __global__ __launch_bounds__(JOIN_THREADS) void join_tree_kernel(TreeArgs a, int rows_of_block, int keys_of_tile, const int32_t *__restrict__ n_valid,
-                                                                 const float *__restrict__ part, const float2 *__restrict__ stats, char *__restrict__ out) {
+                                                                 const float *__restrict__ part, const float2 *__restrict__ stats, char *__restrict__ out,
+                                                                 const char *__restrict__ kn, const char *__restrict__ vn, const int32_t *__restrict__ parent,
+                                                                 char *__restrict__ kc, char *__restrict__ vc) {
   constexpr int COLS = D / 4, AHEAD = 4, SLOTS = JOIN_THREADS / COLS, AT_ONCE = SLOTS / GROUPS, ES = DT == DT_F32 ? 4 : 2;
   __shared__ float4 o_s[GROUPS > 1 ? SLOTS : 1][COLS];
   __shared__ float2 ml_s[GROUPS > 1 ? SLOTS : 1];
   const int bh = blockIdx.x, b = divide(bh, a.kv_magic), h = bh - b * a.Hkv;
-  const int slot = threadIdx.x / COLS, col = threadIdx.x % COLS, group = slot % GROUPS;
-  const int row = blockIdx.y * AT_ONCE + slot / GROUPS, block = row / rows_of_block;
-  const bool exists = row < a.n_rows;
   const int n = load_scalar(n_valid + bh);
   const bool fits = n >= 0 && n <= a.capacity - a.T;
-  const int tiles = fits ? (n + keys_of_tile - 1) / keys_of_tile : 0, splits = max((tiles + a.chunk - 1) / a.chunk, 1);
-  const int64_t at = ((int64_t)bh * a.blocks + block) * a.splits * rows_of_block + (row - block * rows_of_block);
+  if (blockIdx.y == 0) {                     // the new rows go into the cache
+    if (fits) copy_rows<D * ES / 16, JOIN_THREADS>(a, Nodes(a, parent, b).all, b, h, n, kn, vn, kc, vc);
+    return;
+  }
+  const int slot = threadIdx.x / COLS, col = threadIdx.x % COLS, group = slot % GROUPS;
+  const int row = (blockIdx.y - 1) * AT_ONCE + slot / GROUPS, block = row / rows_of_block;
+  const bool exists = row < a.n_rows;
+  // the nodes', then the ranges that hold rows
+  const int tiles = fits ? (n + keys_of_tile - 1) / keys_of_tile : 0, splits = (tiles + a.chunk - 1) / a.chunk + 1;
+  const int64_t at = ((int64_t)bh * a.blocks + block) * (a.splits + 1) * rows_of_block + (row - block * rows_of_block);
   float m = -INFINITY, l = 0.0f, first = 0.0f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   if (exists) first = stats[at].y;
@@ -442,15 +463,20 @@ hipError_t launch_shares(const TreePlan &plan, const void *q, const void *kn, co
   const TreeArgs &a = plan.args;
   float *part = (float *)ws;
   float2 *stats = (float2 *)((char *)ws + plan.stats_at);
-  // (y == splits: the workgroups that put the new rows into the caches)
-  hipLaunchKernelGGL((tree_kernel<D, DT, ROW_WAVES, KEY_WAVES>), dim3((uint32_t)a.heads, (uint32_t)a.splits + 1, (uint32_t)a.blocks), dim3(S::NT), 0, stream, a,
-                     (const char *)q, (const char *)kn, (const char *)vn, parent, (char *)kc, (char *)vc, n_valid, (char *)out, part, stats);
+  const dim3 grid((uint32_t)a.heads, (uint32_t)(a.splits == 1 ? 1 : a.splits + 1), (uint32_t)a.blocks);
+#define WKV_TREE(STREAM) \
+  hipLaunchKernelGGL((tree_kernel<D, DT, ROW_WAVES, KEY_WAVES, STREAM>), grid, dim3(S::NT), 0, stream, a, (const char *)q, (const char *)kn, (const char *)vn, \
+                     parent, (char *)kc, (char *)vc, n_valid, (char *)out, part, stats)
+  if (plan.streams) WKV_TREE(true);
+  else WKV_TREE(false);
+#undef WKV_TREE
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
   constexpr int SLOTS = JOIN_THREADS / (D / 4);
 #define WKV_JOIN(GROUPS) \
-  hipLaunchKernelGGL((join_tree_kernel<D, DT, GROUPS>), dim3((uint32_t)a.heads, (uint32_t)((a.n_rows + SLOTS / GROUPS - 1) / (SLOTS / GROUPS))), \
-                     dim3(JOIN_THREADS), 0, stream, a, S::ROWS, S::KEYS, n_valid, part, stats, (char *)out)
+  hipLaunchKernelGGL((join_tree_kernel<D, DT, GROUPS>), dim3((uint32_t)a.heads, (uint32_t)((a.n_rows + SLOTS / GROUPS - 1) / (SLOTS / GROUPS)) + 1), \
+                     dim3(JOIN_THREADS), 0, stream, a, S::ROWS, S::KEYS, n_valid, part, stats, (char *)out, (const char *)kn, \
+                     (const char *)vn, parent, (char *)kc, (char *)vc)
   if (a.splits > 8) WKV_JOIN(8);
   else WKV_JOIN(1);
 #undef WKV_JOIN
@@ -464,10 +490,7 @@ hipError_t launch_d(const TreePlan &plan, const void *q, const void *kn, const v
   if (plan.row_waves == R && plan.key_waves == K) return launch_shares<D, DT, R, K>(plan, q, kn, vn, parent, kc, vc, n_valid, out, ws, stream)
   WKV_SHARES(2, 2);
   WKV_SHARES(4, 1);
-  if constexpr (DT != DT_F32) {
-    WKV_SHARES(1, 4);
-    WKV_SHARES(8, 1);
-  }
+  if constexpr (DT != DT_F32) WKV_SHARES(8, 1);
 #undef WKV_SHARES
   return hipErrorInvalidValue;
 }
@@ -484,30 +507,35 @@ __device__ __forceinline__ int accepted(const TreeArgs &a, const int32_t *__rest
 }
 
 constexpr int ACCEPT_THREADS = 256;
-// Rows n + path[i] of one tensor and (sequence, KV head) into rows n + i; all are read before the first is written.
+// Rows n + path[i] of one tensor and (sequence, KV head) into rows n + i.  All nodes' rows are asked for before the path is known, and every thread finds out
+// where its own go: two trips to memory instead of three.
 template <int PPR>
 __global__ __launch_bounds__(ACCEPT_THREADS) void accept_kernel(TreeArgs a, EvictLayers layers, const int32_t *__restrict__ path,
                                                                 const int32_t *__restrict__ n_accept, const int32_t *__restrict__ n_valid) {
   constexpr int ROWS = ACCEPT_THREADS / PPR, TURNS = WKV_MAX_NODES / ROWS;
+  __shared__ int place_s[WKV_MAX_NODES];          // of a node's row
   const int bh = blockIdx.x, b = divide(bh, a.kv_magic), h = bh - b * a.Hkv, layer = blockIdx.y >> 1;
   char *cache = (char *)(blockIdx.y & 1 ? layers.v[layer] : layers.k[layer]);
   const int n = load_scalar(n_valid + bh);
-  int node;
-  const int count = accepted(a, path, n_accept, b, node);
   if (n < 0 || n > a.capacity - a.T) return;
   char *rows = cache + (b * a.c_sb + h * a.c_sh + (int64_t)n * a.c_st) + threadIdx.x % PPR * 16;
+  const int my_node = threadIdx.x / PPR;
   uint4 x[TURNS];
-  bool moves[TURNS];
 #pragma unroll
-  for (int k = 0; k < TURNS; ++k) {
-    const int i = k * ROWS + threadIdx.x / PPR, from = __shfl(node, i & 63);
-    moves[k] = i < count && from != i;
-    if (moves[k]) x[k] = *(const uint4 *)(rows + from * a.c_st);
+  for (int k = 0; k < TURNS; ++k)
+    if (k * ROWS + my_node < a.T) x[k] = *(const uint4 *)(rows + (k * ROWS + my_node) * a.c_st);
+  if (threadIdx.x < 64) {
+    place_s[threadIdx.x] = -1;
+    int node;
+    const int count = accepted(a, path, n_accept, b, node);
+    if ((int)threadIdx.x < count) place_s[node] = threadIdx.x;
   }
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < TURNS; ++k)
-    if (moves[k]) *(uint4 *)(rows + (k * ROWS + threadIdx.x / PPR) * a.c_st) = x[k];
+  for (int k = 0; k < TURNS; ++k) {
+    const int t = k * ROWS + my_node, to = place_s[t];
+    if (to >= 0 && to != t) *(uint4 *)(rows + to * a.c_st) = x[k];
+  }
 }
 
 // (a launch of its own: the workgroups above read the counts)

@@ -155,7 +155,7 @@ def tree(fields=None, **kw):
     (dict(n_nodes=0), INVALID), (dict(n_nodes=65), UNSUPPORTED), (dict(capacity=0), INVALID), (dict(capacity=(1 << 30) + 1), UNSUPPORTED), (dict(dtype=-1), INVALID),
     (dict(flags=2), INVALID), (dict(batch=9000), UNSUPPORTED), (dict(scale=-1.0), INVALID), (dict(scale=math.inf), INVALID),
     (dict(cache_strides=(8, 8, 8)), INVALID), (dict(cache_strides=(0, 128, 1 << 24)), UNSUPPORTED), (dict(q_strides=(0, 128, 100)), INVALID),
-    (dict(new_strides=(0, 64, 128)), INVALID), (dict(out_strides=(0, 128, 1 << 50)), INVALID)])
+    (dict(new_strides=(0, 64, 128)), INVALID), (dict(new_strides=(0, 128, 1 << 24)), UNSUPPORTED), (dict(out_strides=(0, 128, 1 << 50)), INVALID)])
 def test_tree_shapes(kw, status):
     sh, lib = tree(**kw), W.lib()
     assert lib.wkv_tree_workspace_bytes(sh.ref()) == 0
