@@ -16,14 +16,27 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false); }
 
-// Where row number i of a launch lies: its (sequence, KV head), its own number r, and its place in the cache (-1: none).
-struct RowOf {
-  int bh, r, place;
-  __device__ __forceinline__ RowOf(const QuantizedArgs &a, uint32_t i) {
-    bh = (int)(i / (uint32_t)a.n_rows);
-    r = (int)(i - (uint32_t)bh * (uint32_t)a.n_rows);
-    const int64_t at = (int64_t)(a.first ? a.first[bh] : 0) + r;
-    place = at >= 0 && at < a.capacity ? (int)at : -1;
+// Where the rows of a lane lie, every UNITS-th of the launch from row i0 on: its (sequence, KV head), its own number r, and its place in the cache (-1: none).
+// Everything that is looked up for all of them is asked for at once: row by row, each with its own trips to memory, the 4128 kept rows of the 32K benchmark's prompt in four
+// layers took 37 us.
+template <int UNITS>
+struct RowsOf {
+  int bh[AT_ONCE], r[AT_ONCE], place[AT_ONCE];
+  __device__ __forceinline__ RowsOf(const QuantizedArgs &a, int64_t i0) {
+    const int64_t total = (int64_t)a.heads * a.n_rows;
+    int first[AT_ONCE];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const uint32_t i = (uint32_t)min(i0 + u * UNITS, total - 1);
+      bh[u] = (int)(i / (uint32_t)a.n_rows);
+      r[u] = (int)(i - (uint32_t)bh[u] * (uint32_t)a.n_rows);
+      first[u] = a.first ? a.first[bh[u]] : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const int64_t at = (int64_t)first[u] + r[u];
+      place[u] = i0 + u * UNITS < total && at >= 0 && at < a.capacity ? (int)at : -1;
+    }
   }
 };
 
@@ -34,35 +47,31 @@ __global__ __launch_bounds__(QZ_THREADS) void quantize_kernel(QuantizedArgs a, Q
   const char *plain = (const char *)layers.plain[is_v][layer];
   char *codes = (char *)layers.codes[is_v][layer], *scales = (char *)layers.scales[is_v][layer];
   const int lane = threadIdx.x % LPR, unit = threadIdx.x / LPR;
-  const int64_t total = (int64_t)a.heads * a.n_rows, i0 = (int64_t)blockIdx.x * (UNITS * AT_ONCE) + unit;
+  const int64_t i0 = (int64_t)blockIdx.x * (UNITS * AT_ONCE) + unit;
 
-  uint4 x[AT_ONCE][PIECES];
-  int bh[AT_ONCE], place[AT_ONCE];
+  RowsOf<UNITS> rows(a, i0);
+  int keep[AT_ONCE], from[AT_ONCE];
 #pragma unroll
   for (int u = 0; u < AT_ONCE; ++u) {
-    const int64_t i = i0 + u * UNITS;
-    place[u] = -1;
-    if (i >= total) continue;
-    const RowOf row(a, (uint32_t)i);
-    bh[u] = row.bh;
-    place[u] = a.n_keep && row.r >= a.n_keep[row.bh] ? -1 : row.place;
-    int from = row.r;
-    if (a.tok_idx) {
-      from = a.tok_idx[i];
-      if (from < 0 || from >= a.row_capacity) place[u] = -1;
-    }
-    if (place[u] < 0) continue;
-    const int b = divide((uint32_t)row.bh, a.kv_magic), h = row.bh - b * a.Hkv;
-    const char *in = plain + (b * a.r_sb + h * a.r_sh + from * a.r_st) + lane * (16 * PIECES);
+    keep[u] = a.n_keep ? a.n_keep[rows.bh[u]] : a.n_rows;
+    from[u] = a.tok_idx ? a.tok_idx[(int64_t)rows.bh[u] * a.n_rows + rows.r[u]] : rows.r[u];
+  }
+  u32x4 x[AT_ONCE][PIECES];
 #pragma unroll
-    for (int k = 0; k < PIECES; ++k) x[u][k] = *(const uint4 *)(in + k * 16);
+  for (int u = 0; u < AT_ONCE; ++u) {
+    if (rows.r[u] >= keep[u] || from[u] < 0 || from[u] >= a.row_capacity) rows.place[u] = -1;
+    const int b = divide((uint32_t)rows.bh[u], a.kv_magic), h = rows.bh[u] - b * a.Hkv;
+    const char *in = plain + (b * a.r_sb + h * a.r_sh + from[u] * a.r_st) + lane * (16 * PIECES);
+    if (rows.place[u] >= 0)
+#pragma unroll
+      for (int k = 0; k < PIECES; ++k) x[u][k] = *(const u32x4 *)(in + k * 16);
   }
 #pragma unroll
   for (int u = 0; u < AT_ONCE; ++u) {
-    if (place[u] < 0) continue;                  // (the same in all lanes of a row)
+    if (rows.place[u] < 0) continue;             // (the same in all lanes of a row)
     float f[8];
-    widen<DT>(x[u][0], f);
-    if constexpr (PIECES == 2) widen<DT>(x[u][1], f + 4);
+    widen<DT>(__builtin_bit_cast(uint4, x[u][0]), f);
+    if constexpr (PIECES == 2) widen<DT>(__builtin_bit_cast(uint4, x[u][1]), f + 4);
     uint32_t largest = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) largest = max(largest, __float_as_uint(f[e]) & 0x7fffffffu);
@@ -70,8 +79,8 @@ __global__ __launch_bounds__(QZ_THREADS) void quantize_kernel(QuantizedArgs a, Q
     largest = max(largest, dpp<0x4E>(largest));                  // quad_perm [2,3,0,1]
     const uint32_t byte = (uint32_t)scale_byte<FORMAT>(largest);
     const float scale = scale_of(byte);
-    const int b = divide((uint32_t)bh[u], a.kv_magic), h = bh[u] - b * a.Hkv;
-    char *to = codes + (b * a.c_sb + h * a.c_sh + place[u] * a.c_st);
+    const int b = divide((uint32_t)rows.bh[u], a.kv_magic), h = rows.bh[u] - b * a.Hkv;
+    char *to = codes + (b * a.c_sb + h * a.c_sh + rows.place[u] * a.c_st);
     if constexpr (FORMAT == E4M3) {
       uint32_t lo = to_codes<FORMAT, 1>(to_codes<FORMAT, 0>(0, f[0], f[1], scale), f[2], f[3], scale);
       uint32_t hi = to_codes<FORMAT, 1>(to_codes<FORMAT, 0>(0, f[4], f[5], scale), f[6], f[7], scale);
@@ -84,7 +93,7 @@ __global__ __launch_bounds__(QZ_THREADS) void quantize_kernel(QuantizedArgs a, Q
       *(uint32_t *)(to + lane * 4) = w;
     }
     uint32_t all = byte << (lane / 4 * 8);
-    char *sc = scales + ((int64_t)bh[u] * a.capacity + place[u]) * SB;
+    char *sc = scales + ((int64_t)rows.bh[u] * a.capacity + rows.place[u]) * SB;
     if constexpr (D == 128) {
       all |= dpp<0x124>(all);                                    // row_ror:4
       all |= dpp<0x128>(all);                                    // row_ror:8
@@ -104,23 +113,25 @@ __global__ __launch_bounds__(QZ_THREADS) void dequantize_kernel(QuantizedArgs a,
   const char *codes = (const char *)layers.codes[is_v][layer];
   const uint8_t *scales = (const uint8_t *)layers.scales[is_v][layer];
   const int lane = threadIdx.x % LPR, unit = threadIdx.x / LPR;
-  const int64_t total = (int64_t)a.heads * a.n_rows, i0 = (int64_t)blockIdx.x * (UNITS * AT_ONCE) + unit;
+  const int64_t i0 = (int64_t)blockIdx.x * (UNITS * AT_ONCE) + unit;
 
+  RowsOf<UNITS> rows(a, i0);
+  int valid[AT_ONCE];
+#pragma unroll
+  for (int u = 0; u < AT_ONCE; ++u) valid[u] = a.n_keep ? a.n_keep[rows.bh[u]] : a.capacity;
   uint32_t x[AT_ONCE][WORDS], byte[AT_ONCE];
   char *to[AT_ONCE];
 #pragma unroll
   for (int u = 0; u < AT_ONCE; ++u) {
-    const int64_t i = i0 + u * UNITS;
-    to[u] = nullptr;
-    if (i >= total) continue;
-    const RowOf row(a, (uint32_t)i);
-    if (row.place < 0 || (a.n_keep && row.place >= a.n_keep[row.bh])) continue;
-    const int b = divide((uint32_t)row.bh, a.kv_magic), h = row.bh - b * a.Hkv;
-    const char *in = codes + (b * a.c_sb + h * a.c_sh + row.place * a.c_st) + lane * (WORDS * 4);
-    if constexpr (WORDS == 2) { const u32x2 w = *(const u32x2 *)in; x[u][0] = w[0]; x[u][1] = w[1]; }
-    else x[u][0] = *(const uint32_t *)in;
-    byte[u] = scales[((int64_t)row.bh * a.capacity + row.place) * SB + lane / 4];
-    to[u] = plain + (b * a.r_sb + h * a.r_sh + row.r * a.r_st) + lane * (DT == DT_F32 ? 32 : 16);
+    if (rows.place[u] >= valid[u]) rows.place[u] = -1;
+    const int b = divide((uint32_t)rows.bh[u], a.kv_magic), h = rows.bh[u] - b * a.Hkv;
+    const char *in = codes + (b * a.c_sb + h * a.c_sh + rows.place[u] * a.c_st) + lane * (WORDS * 4);
+    if (rows.place[u] >= 0) {
+      if constexpr (WORDS == 2) { const u32x2 w = *(const u32x2 *)in; x[u][0] = w[0]; x[u][1] = w[1]; }
+      else x[u][0] = *(const uint32_t *)in;
+      byte[u] = scales[((int64_t)rows.bh[u] * a.capacity + rows.place[u]) * SB + lane / 4];
+    }
+    to[u] = rows.place[u] < 0 ? nullptr : plain + (b * a.r_sb + h * a.r_sh + rows.r[u] * a.r_st) + lane * (DT == DT_F32 ? 32 : 16);
   }
 #pragma unroll
   for (int u = 0; u < AT_ONCE; ++u) {

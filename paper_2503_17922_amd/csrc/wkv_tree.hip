@@ -16,6 +16,8 @@ namespace wkv {
 
 namespace {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 // The nodes of a sequence, one to a lane.
 struct Nodes {
   uint64_t family, all;          // this lane's node: itself and those it hangs below (0: it does not exist); which nodes exist
@@ -66,16 +68,16 @@ __device__ __forceinline__ void copy_rows(const TreeArgs &a, uint64_t all, int b
   constexpr int AHEAD = 4;
   const int64_t from = b * a.n_sb + h * a.n_sh, to = b * a.c_sb + h * a.c_sh + n * a.c_st;
   for (int i0 = threadIdx.x; i0 < 2 * a.T * PPR; i0 += AHEAD * NT) {
-    uint4 x[AHEAD];
+    u32x4 x[AHEAD];
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
       const int i = min(i0 + k * NT, 2 * a.T * PPR - 1), r = i / PPR;
-      x[k] = *(const uint4 *)((r & 1 ? vn : kn) + from + (r >> 1) * a.n_st + i % PPR * 16);
+      x[k] = *(const u32x4 *)((r & 1 ? vn : kn) + from + (r >> 1) * a.n_st + i % PPR * 16);
     }
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
       const int i = i0 + k * NT, r = i / PPR;
-      if (i < 2 * a.T * PPR && all >> (r >> 1) & 1) *(uint4 *)((r & 1 ? vc : kc) + to + (r >> 1) * a.c_st + i % PPR * 16) = x[k];
+      if (i < 2 * a.T * PPR && all >> (r >> 1) & 1) *(u32x4 *)((r & 1 ? vc : kc) + to + (r >> 1) * a.c_st + i % PPR * 16) = x[k];
     }
   }
 }
@@ -520,10 +522,10 @@ __global__ __launch_bounds__(ACCEPT_THREADS) void accept_kernel(TreeArgs a, Evic
   if (n < 0 || n > a.capacity - a.T) return;
   char *rows = cache + (b * a.c_sb + h * a.c_sh + (int64_t)n * a.c_st) + threadIdx.x % PPR * 16;
   const int my_node = threadIdx.x / PPR;
-  uint4 x[TURNS];
+  u32x4 x[TURNS];
 #pragma unroll
   for (int k = 0; k < TURNS; ++k)
-    if (k * ROWS + my_node < a.T) x[k] = *(const uint4 *)(rows + (k * ROWS + my_node) * a.c_st);
+    x[k] = *(const u32x4 *)(rows + min(k * ROWS + my_node, a.T - 1) * a.c_st);          // (without a condition, under which an array leaves the registers)
   if (threadIdx.x < 64) {
     place_s[threadIdx.x] = -1;
     int node;
@@ -534,7 +536,7 @@ __global__ __launch_bounds__(ACCEPT_THREADS) void accept_kernel(TreeArgs a, Evic
 #pragma unroll
   for (int k = 0; k < TURNS; ++k) {
     const int t = k * ROWS + my_node, to = place_s[t];
-    if (to >= 0 && to != t) *(uint4 *)(rows + to * a.c_st) = x[k];
+    if (to >= 0 && to != t) *(u32x4 *)(rows + to * a.c_st) = x[k];
   }
 }
 
