@@ -35,6 +35,15 @@ template <> struct Word<4> { typedef uint32_t type; };
 template <> struct Word<8> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
 template <> struct Word<16> { typedef uint32_t type __attribute__((ext_vector_type(4))); };
 
+// STREAM: a nontemporal load, which puts nothing into the memory-side cache.
+typedef const __attribute__((address_space(1))) char *global_ptr;
+template <bool STREAM, typename T>
+__device__ __forceinline__ T load(global_ptr base, uint32_t offset) {
+  typedef const __attribute__((address_space(1))) T *P;
+  if constexpr (STREAM) return __builtin_nontemporal_load((P)(base + offset));
+  else return *(P)(base + offset);
+}
+
 // Word w of a load.
 template <typename T>
 __device__ __forceinline__ uint32_t word(const T &x, int w) {
@@ -60,6 +69,9 @@ __device__ __forceinline__ uint32_t part_of(float a, float b, int which) {
   return which < N ? got : 0u;
 }
 
+// A number's upper eight bits.
+__device__ __forceinline__ float upper(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+
 // The sum over the columns of a head, in all of them: lanes COLUMNS apart within 16.
 template <int COLUMNS>
 __device__ __forceinline__ float columns_sum(float x) {
@@ -69,7 +81,7 @@ __device__ __forceinline__ float columns_sum(float x) {
 }
 
 // COLUMNS: 4 or 8 heads at most, in this many columns; 16 / COLUMNS parts of a number fit beside each other.
-template <int DT, int D, int FORMAT, int COLUMNS>
+template <int DT, int D, int FORMAT, int COLUMNS, bool STREAM>
 __global__ __launch_bounds__(DQ_THREADS, 2) void decode_quantized_kernel(DecodeShape s, const char *__restrict__ q_new, const char *__restrict__ k_codes,
                                                                         const uint8_t *__restrict__ k_scales, const char *__restrict__ v_codes,
                                                                         const uint8_t *__restrict__ v_scales, const int32_t *__restrict__ n_valid,
@@ -102,26 +114,34 @@ __global__ __launch_bounds__(DQ_THREADS, 2) void decode_quantized_kernel(DecodeS
     typename Word<R::V_LOAD>::type v[8];
     uint32_t k_scale[2], v_scale[2];
   };
-  auto request = [&](Raw &x, int j) __attribute__((always_inline)) {
-    const int j0 = min(j, cend - 1), last = cend - 1 - j0;          // rows past the range: its last one again
-    const char *kb = kc + (int64_t)j0 * s.st, *vb = vc + (int64_t)j0 * s.st;
-    const uint8_t *ksb = ks + (int64_t)j0 * R::SB, *vsb = vs + (int64_t)j0 * R::SB;
+  const uint32_t k_row = col * st, v_row = quad * 4 * st, ks_row = col * R::SB, vs_row = (quad * 4 + (col & 3)) * R::SB;
+  const uint32_t k_lane = quad * R::K_LOAD, v_lane = col * R::V_LOAD, vs_lane = col * R::V_CH / SCALE_GROUP;
+  auto request = [&](Raw &x, int j0) __attribute__((always_inline)) {
+    typedef typename Word<R::K_LOAD>::type KW;
+    typedef typename Word<R::V_LOAD>::type VW;
+    typedef typename Word<R::SB>::type SW;
+    global_ptr kb = (global_ptr)(kc + (int64_t)j0 * s.st), vb = (global_ptr)(vc + (int64_t)j0 * s.st);
+    global_ptr ksb = (global_ptr)(ks + (int64_t)j0 * R::SB), vsb = (global_ptr)(vs + (int64_t)j0 * R::SB);
+    // (a scalar address and an offset of 32 bits each: left to itself the compiler keeps 64 bits a load and lane)
+    asm("" : "+s"(kb));
+    asm("" : "+s"(vb));
+    asm("" : "+s"(ksb));
+    asm("" : "+s"(vsb));
+    const uint32_t last = min(cend - 1 - j0, BLOCK - 1), most = last * st;          // rows past the range: its last one again
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const uint32_t r = min(t * 16 + col, last);
+      const uint32_t at = min(k_row + t * 16 * st, most) + k_lane;
 #pragma unroll
-      for (int l = 0; l < R::K_LOADS; ++l)
-        x.k[t][l] = *(const typename Word<R::K_LOAD>::type *)(kb + r * st + (l * 4 + quad) * R::K_LOAD);
-      x.k_scale[t] = *(const typename Word<R::SB>::type *)(ksb + r * R::SB);
+      for (int l = 0; l < R::K_LOADS; ++l) x.k[t][l] = load<STREAM, KW>(kb, at + l * 4 * R::K_LOAD);
+      x.k_scale[t] = load<false, SW>(ksb, min(ks_row + t * 16 * R::SB, last * R::SB));
       // a quad of lanes has the scales of its channels in four rows
-      x.v_scale[t] = vsb[min(t * 16 + quad * 4 + (col & 3), last) * R::SB + col * R::V_CH / SCALE_GROUP];
+      x.v_scale[t] = load<false, uint8_t>(vsb, min(vs_row + t * 16 * R::SB, last * R::SB) + vs_lane);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      x.v[i] = *(const typename Word<R::V_LOAD>::type *)(vb + (uint32_t)min(i / 4 * 16 + quad * 4 + i % 4, last) * st + col * R::V_LOAD);
+    for (int i = 0; i < 8; ++i) x.v[i] = load<STREAM, VW>(vb, min(v_row + (i / 4 * 16 + i % 4) * st, most) + v_lane);
   };
   Raw next;
-  request(next, c0 + wave * BLOCK);
+  if (c0 + wave * BLOCK < cend) request(next, c0 + wave * BLOCK);
 
   // ---- queries: B fragments
   bf16x8 qf[Q_SETS][QS];
@@ -146,6 +166,9 @@ __global__ __launch_bounds__(DQ_THREADS, 2) void decode_quantized_kernel(DecodeS
       }
     }
 
+  // COLUMNS == 4: parts 0, 1, 2 of a probability, and its third part's rest, which is nothing; 8: parts 0 and 1, then part 2 in the first eight columns
+  const float takes_first = which >= 1 ? 1.0f : 0.0f, takes_second = which >= 2 ? 1.0f : 0.0f, takes_third = which == 0 ? 1.0f : 0.0f;
+  const float nothing = COLUMNS == 4 && which == 3 ? -INFINITY : 0.0f;          // added to a logit
   f32x4 o[R::V_CH];                          // o[c][i]: channel (quad * 4 + i) * V_CH + c, of this column
 #pragma unroll
   for (int c = 0; c < R::V_CH; ++c) o[c] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
@@ -153,7 +176,7 @@ __global__ __launch_bounds__(DQ_THREADS, 2) void decode_quantized_kernel(DecodeS
 
   for (int j0 = c0 + wave * BLOCK; j0 < cend; j0 += DQ_WAVES * BLOCK) {
     const Raw x = next;
-    request(next, j0 + DQ_WAVES * BLOCK);
+    if (j0 + DQ_WAVES * BLOCK < cend) request(next, j0 + DQ_WAVES * BLOCK);
     // ---- logits of 32 rows: element i of tile t is row t * 16 + quad * 4 + i
     f32x4 sc[2];
 #pragma unroll
@@ -178,15 +201,19 @@ __global__ __launch_bounds__(DQ_THREADS, 2) void decode_quantized_kernel(DecodeS
         }
       }
     }
-    float p[8], top = -INFINITY;
+    float p[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      p[i] = columns_sum<COLUMNS>(sc[i / 4][i % 4]) * s.c1;
-      if (j0 + i / 4 * 16 + quad * 4 + i % 4 >= cend) p[i] = -INFINITY;
-      top = fmaxf(top, p[i]);
+    for (int i = 0; i < 8; ++i) p[i] = columns_sum<COLUMNS>(sc[i / 4][i % 4]);
+    if (j0 + BLOCK > cend) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (j0 + i / 4 * 16 + quad * 4 + i % 4 >= cend) p[i] = -INFINITY;
     }
+    float top = p[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) top = fmaxf(top, p[i]);
     // (the reference is the same in all lanes of a column, and moves when a logit is 2^8 times as much)
-    top = quads_max(top);
+    top = quads_max(top) * s.c1;
     if (__any(top > m + 8.0f)) {
       const float to = fmaxf(m, top), corr = to == -INFINITY ? 1.0f : fast_exp2(m - to);
       m = to;
@@ -197,16 +224,33 @@ __global__ __launch_bounds__(DQ_THREADS, 2) void decode_quantized_kernel(DecodeS
     const float ref = m == -INFINITY ? 0.0f : m;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      p[i] = fast_exp2(p[i] - ref);
+      p[i] = fast_exp2(fmaf(p[i], s.c1, nothing - ref));
       l += p[i];
     }
+    // Three parts of a probability, its upper eight bits, the next eight and the last: cut off, so that their sum is the number itself.  Every lane goes as far as its part.
     bf16x8 pf[P_SETS];
+    {
+      float x0[8], x1[8];
 #pragma unroll
-    for (int set = 0; set < P_SETS; ++set) {
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (COLUMNS == 4) {
+          x0[i] = fmaf(-takes_first, upper(p[i]), p[i]);
+          x0[i] = fmaf(-takes_second, upper(x0[i]), x0[i]);
+        } else {
+          const float rest = p[i] - upper(p[i]);
+          x0[i] = which ? rest : p[i];
+          x1[i] = (rest - upper(rest)) * takes_third;
+        }
+      }
       uint32_t w[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = part_of<PARTS>(p[2 * i], p[2 * i + 1], set * FIT + which);
-      pf[set] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+      for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_perm(__float_as_uint(x0[2 * i + 1]), __float_as_uint(x0[2 * i]), 0x07060302u);
+      pf[0] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+      if constexpr (P_SETS == 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_perm(__float_as_uint(x1[2 * i + 1]), __float_as_uint(x1[2 * i]), 0x07060302u);
+        pf[1] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+      }
     }
     // ---- values: pairs of channels of a row, then pairs of rows of a channel
     uint32_t vf[R::V_CH][4];
@@ -217,12 +261,13 @@ __global__ __launch_bounds__(DQ_THREADS, 2) void decode_quantized_kernel(DecodeS
       for (int k = 0; k < 2; ++k) {
         const int i = 2 * r + k;
         // row i's scale lies in lane i % 4 of every quad
+        const int from = (int)x.v_scale[i / 4];
         uint32_t byte;
         switch (i % 4) {
-          case 0: byte = __builtin_amdgcn_update_dpp(0, (int)x.v_scale[i / 4], 0x00, 0xF, 0xF, false); break;
-          case 1: byte = __builtin_amdgcn_update_dpp(0, (int)x.v_scale[i / 4], 0x55, 0xF, 0xF, false); break;
-          case 2: byte = __builtin_amdgcn_update_dpp(0, (int)x.v_scale[i / 4], 0xAA, 0xF, 0xF, false); break;
-          default: byte = __builtin_amdgcn_update_dpp(0, (int)x.v_scale[i / 4], 0xFF, 0xF, 0xF, false); break;
+          case 0: byte = __builtin_amdgcn_mov_dpp(from, 0x00, 0xF, 0xF, true); break;
+          case 1: byte = __builtin_amdgcn_mov_dpp(from, 0x55, 0xF, 0xF, true); break;
+          case 2: byte = __builtin_amdgcn_mov_dpp(from, 0xAA, 0xF, 0xF, true); break;
+          default: byte = __builtin_amdgcn_mov_dpp(from, 0xFF, 0xF, 0xF, true); break;
         }
         const float scale = scale_of(byte);
         if constexpr (FORMAT == E4M3) {
@@ -258,10 +303,12 @@ __global__ __launch_bounds__(DQ_THREADS, 2) void decode_quantized_kernel(DecodeS
 #pragma unroll
   for (int c = 0; c < R::V_CH; ++c)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float x = columns_sum<COLUMNS>(o[c][i]);
-      if (col < COLUMNS) wave_state[wave][col][(quad * 4 + i) * R::V_CH + c] = x;
-    }
+    for (int i = 0; i < 4; ++i) o[c][i] = columns_sum<COLUMNS>(o[c][i]);
+  if (col < COLUMNS)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < R::V_CH; ++c) wave_state[wave][col][(quad * 4 + i) * R::V_CH + c] = o[c][i];
   if (quad == 0 && col < COLUMNS) { wave_state[wave][col][D] = m; wave_state[wave][col][D + 1] = l; }
   __syncthreads();
   for (int i = threadIdx.x; i < s.G * D; i += DQ_THREADS) {
@@ -387,11 +434,13 @@ template <int DT, int D, int FORMAT>
 hipError_t launch_as(const DecodeShape &s, const void *q, const void *kn, const void *vn, void *kc, void *ks, void *vc, void *vs, int32_t *n_valid, float *out,
                      float *part, hipStream_t stream) {
   const dim3 grid(s.B * s.Hkv, s.n_splits);
-#define WKV_DQ(COLUMNS) \
-  hipLaunchKernelGGL((decode_quantized_kernel<DT, D, FORMAT, COLUMNS>), grid, dim3(DQ_THREADS), 0, stream, s, (const char *)q, (const char *)kc, \
+  // what exceeds the memory-side cache is not found there at the next token
+  const bool streams = 2 * (int64_t)s.B * s.Hkv * s.capacity * (code_bytes<FORMAT>(D) + D / SCALE_GROUP) > MEMORY_CACHE_BYTES;
+#define WKV_DQ(COLUMNS, STREAM) \
+  hipLaunchKernelGGL((decode_quantized_kernel<DT, D, FORMAT, COLUMNS, STREAM>), grid, dim3(DQ_THREADS), 0, stream, s, (const char *)q, (const char *)kc, \
                      (const uint8_t *)ks, (const char *)vc, (const uint8_t *)vs, n_valid, part)
-  if (s.G <= 4) WKV_DQ(4);
-  else WKV_DQ(8);
+  if (s.G <= 4) { if (streams) WKV_DQ(4, true); else WKV_DQ(4, false); }
+  else { if (streams) WKV_DQ(8, true); else WKV_DQ(8, false); }
 #undef WKV_DQ
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
