@@ -244,7 +244,7 @@ wkv_status wkv_cache_quantize(const wkv_quantized_shape *shape, int32_t n_layers
   if (shape->row_capacity < (tok_idx ? 0 : a.n_rows)) return invalid("row_capacity must be >= n_rows, or >= 0 with tok_idx");
   if (misaligned(tok_idx, 4) || misaligned(n_keep, 4) || misaligned(first, 4)) return invalid("tok_idx, n_keep and first must be 4-byte aligned");
   a.tok_idx = tok_idx; a.n_keep = n_keep; a.first = first;
-  if (a.n_rows == 0) return WKV_OK;
+  if (a.n_rows == 0 || a.row_capacity == 0) return WKV_OK;
   return launched(launch_quantize(a, layers, n_layers, (hipStream_t)hip_stream), "wkv_cache_quantize");
 }
 

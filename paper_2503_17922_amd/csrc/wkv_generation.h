@@ -30,6 +30,8 @@ struct QuantizedArgs {
   uint32_t kv_magic;                           // division_magic(Hkv)
   int64_t c_sb, c_sh, c_st, r_sb, r_sh, r_st;  // strides of codes and of plain rows in bytes
   const int32_t *tok_idx, *n_keep, *first;     // wkv_cache_dequantize: n_keep is its n_valid
+  int32_t group;                               // of the launch: (sequence, KV head) pairs to a workgroup; division_magic(n_rows)
+  uint32_t rows_magic;
 };
 hipError_t launch_quantize(const QuantizedArgs &a, const QuantizedLayers &layers, int32_t n_layers, hipStream_t stream);
 hipError_t launch_dequantize(const QuantizedArgs &a, const QuantizedLayers &layers, int32_t n_layers, hipStream_t stream);

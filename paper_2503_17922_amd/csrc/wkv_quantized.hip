@@ -1,74 +1,107 @@
 // Cache rows into 8 and 4 bits and back: bound by memory, which every row crosses once each way.
 //
 // A lane takes eight channels; four lanes share a scale, whose largest magnitude is found by two DPP steps.  The lanes of a row put its scales
-// together, so that they leave in one store.  Rows of all (sequence, KV head) pairs are numbered through, so that a token a sequence fills
-// workgroups as well as a long prompt does.
+// together, so that they leave in one store.  A workgroup takes rows of one (sequence, KV head), whose counts are scalars then, or, where there are
+// few rows to each, all rows of several: a token a sequence fills workgroups as well as a long prompt does.
+//
+// The 4128 kept rows a KV head of the 32K benchmark's prompt, four layers (102 MB), picked one by one from eight times as many: into 8 bits 37 us row by row with a lookup each, 29.5
+// with everything looked up at once, 22.3 = 4.6 TB/s with the plain rows read by nontemporal loads (a plain load leaves them in the memory-side cache, where nobody looks for them); the stores
+// are 8 of it.  Back 17.3 us = 5.9 TB/s.
 #include "wkv_few_bits.h"
 
 namespace wkv {
 
 namespace {
 
-constexpr int QZ_THREADS = 256, AT_ONCE = 4;      // rows of a lane at once
+// Rows of a lane at once.  Two / four / eight, us: a token for each of 64 sequences, four layers, 3.4 / 4.4 / 5.9 into 8 bits, 3.2 / 3.8 / 4.7 back; the long calls above
+// 29.4 / 30.6 / 32.3 and 17.6 / 17.2 / 17.4 (workgroups of 64 to 256 threads the same).
+constexpr int QZ_THREADS = 256, AT_ONCE = 2;
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false); }
 
-// Where the rows of a lane lie, every UNITS-th of the launch from row i0 on: its (sequence, KV head), its own number r, and its place in the cache (-1: none).
-// Everything that is looked up for all of them is asked for at once: row by row, each with its own trips to memory, the 4128 kept rows of the 32K benchmark's prompt in four
-// layers took 37 us.
-template <int UNITS>
+// Where the rows of a lane lie, every UNITS-th of the workgroup's: its (sequence, KV head), its own number r, its place in the cache, and whether there is such a row at all.
+// (No number of a row that is not there leaves its range, so that nothing is loaded under a condition: behind one the compiler waits for each load by itself, which
+// costs a trip to memory a row.)
+// MANY: `group` (sequence, KV head) pairs to a workgroup.
+template <int UNITS, bool MANY>
 struct RowsOf {
   int bh[AT_ONCE], r[AT_ONCE], place[AT_ONCE];
-  __device__ __forceinline__ RowsOf(const QuantizedArgs &a, int64_t i0) {
-    const int64_t total = (int64_t)a.heads * a.n_rows;
+  bool there[AT_ONCE];
+  __device__ __forceinline__ RowsOf(const QuantizedArgs &a, int unit) {
     int first[AT_ONCE];
 #pragma unroll
     for (int u = 0; u < AT_ONCE; ++u) {
-      const uint32_t i = (uint32_t)min(i0 + u * UNITS, total - 1);
-      bh[u] = (int)(i / (uint32_t)a.n_rows);
-      r[u] = (int)(i - (uint32_t)bh[u] * (uint32_t)a.n_rows);
-      first[u] = a.first ? a.first[bh[u]] : 0;
+      const int v = u * UNITS + unit;
+      if constexpr (MANY) {
+        const int at = divide((uint32_t)v, a.rows_magic);
+        there[u] = at < a.group && (int)blockIdx.y * a.group + at < a.heads;
+        bh[u] = min((int)blockIdx.y * a.group + at, a.heads - 1);
+        r[u] = v - at * a.n_rows;
+      } else {
+        bh[u] = blockIdx.y;
+        r[u] = (int)blockIdx.x * (UNITS * AT_ONCE) + v;
+        there[u] = r[u] < a.n_rows;
+        r[u] = min(r[u], a.n_rows - 1);
+      }
     }
+    of(a.first, 0, first);
 #pragma unroll
     for (int u = 0; u < AT_ONCE; ++u) {
       const int64_t at = (int64_t)first[u] + r[u];
-      place[u] = i0 + u * UNITS < total && at >= 0 && at < a.capacity ? (int)at : -1;
+      there[u] = there[u] && at >= 0 && at < a.capacity;
+      place[u] = (int)min(max(at, (int64_t)0), (int64_t)a.capacity - 1);
+    }
+  }
+  // A number of each (sequence, KV head), `otherwise` where there are none.
+  __device__ __forceinline__ void of(const int32_t *p, int otherwise, int (&x)[AT_ONCE]) const {
+    if (!p) {
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) x[u] = otherwise;
+    } else if constexpr (MANY) {
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) x[u] = p[bh[u]];
+    } else {
+      const int all = load_scalar(p + blockIdx.y);
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) x[u] = all;
     }
   }
 };
 
-template <int DT, int D, int FORMAT>
+template <int DT, int D, int FORMAT, bool MANY>
 __global__ __launch_bounds__(QZ_THREADS) void quantize_kernel(QuantizedArgs a, QuantizedLayers layers) {
   constexpr int LPR = D / 8, UNITS = QZ_THREADS / LPR, PIECES = DT == DT_F32 ? 2 : 1, SB = D / SCALE_GROUP;
   const int layer = blockIdx.z >> 1, is_v = blockIdx.z & 1;
   const char *plain = (const char *)layers.plain[is_v][layer];
   char *codes = (char *)layers.codes[is_v][layer], *scales = (char *)layers.scales[is_v][layer];
   const int lane = threadIdx.x % LPR, unit = threadIdx.x / LPR;
-  const int64_t i0 = (int64_t)blockIdx.x * (UNITS * AT_ONCE) + unit;
 
-  RowsOf<UNITS> rows(a, i0);
+  if (!MANY && a.n_keep && (int)blockIdx.x * (UNITS * AT_ONCE) >= load_scalar(a.n_keep + blockIdx.y)) return;
+  RowsOf<UNITS, MANY> rows(a, unit);
   int keep[AT_ONCE], from[AT_ONCE];
+  rows.of(a.n_keep, a.n_rows, keep);
+  if (a.tok_idx) {
 #pragma unroll
-  for (int u = 0; u < AT_ONCE; ++u) {
-    keep[u] = a.n_keep ? a.n_keep[rows.bh[u]] : a.n_rows;
-    from[u] = a.tok_idx ? a.tok_idx[(int64_t)rows.bh[u] * a.n_rows + rows.r[u]] : rows.r[u];
+    for (int u = 0; u < AT_ONCE; ++u) from[u] = a.tok_idx[(int64_t)rows.bh[u] * a.n_rows + rows.r[u]];
+  } else {
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) from[u] = rows.r[u];
   }
   u32x4 x[AT_ONCE][PIECES];
 #pragma unroll
   for (int u = 0; u < AT_ONCE; ++u) {
-    if (rows.r[u] >= keep[u] || from[u] < 0 || from[u] >= a.row_capacity) rows.place[u] = -1;
+    rows.there[u] = rows.there[u] && rows.r[u] < keep[u] && from[u] >= 0 && from[u] < a.row_capacity;
     const int b = divide((uint32_t)rows.bh[u], a.kv_magic), h = rows.bh[u] - b * a.Hkv;
-    const char *in = plain + (b * a.r_sb + h * a.r_sh + from[u] * a.r_st) + lane * (16 * PIECES);
-    if (rows.place[u] >= 0)
+    const char *in = plain + (b * a.r_sb + h * a.r_sh + min(max(from[u], 0), a.row_capacity - 1) * a.r_st) + lane * (16 * PIECES);
 #pragma unroll
-      for (int k = 0; k < PIECES; ++k) x[u][k] = *(const u32x4 *)(in + k * 16);
+    for (int k = 0; k < PIECES; ++k) x[u][k] = __builtin_nontemporal_load((const u32x4 *)(in + k * 16));
   }
 #pragma unroll
   for (int u = 0; u < AT_ONCE; ++u) {
-    if (rows.place[u] < 0) continue;             // (the same in all lanes of a row)
+    if (!rows.there[u]) continue;                // (the same in all lanes of a row)
     float f[8];
     widen<DT>(__builtin_bit_cast(uint4, x[u][0]), f);
     if constexpr (PIECES == 2) widen<DT>(__builtin_bit_cast(uint4, x[u][1]), f + 4);
@@ -105,7 +138,7 @@ __global__ __launch_bounds__(QZ_THREADS) void quantize_kernel(QuantizedArgs a, Q
   }
 }
 
-template <int DT, int D, int FORMAT>
+template <int DT, int D, int FORMAT, bool MANY>
 __global__ __launch_bounds__(QZ_THREADS) void dequantize_kernel(QuantizedArgs a, QuantizedLayers layers) {
   constexpr int LPR = D / 8, UNITS = QZ_THREADS / LPR, SB = D / SCALE_GROUP, WORDS = FORMAT == E4M3 ? 2 : 1;
   const int layer = blockIdx.z >> 1, is_v = blockIdx.z & 1;
@@ -113,29 +146,26 @@ __global__ __launch_bounds__(QZ_THREADS) void dequantize_kernel(QuantizedArgs a,
   const char *codes = (const char *)layers.codes[is_v][layer];
   const uint8_t *scales = (const uint8_t *)layers.scales[is_v][layer];
   const int lane = threadIdx.x % LPR, unit = threadIdx.x / LPR;
-  const int64_t i0 = (int64_t)blockIdx.x * (UNITS * AT_ONCE) + unit;
 
-  RowsOf<UNITS> rows(a, i0);
+  if (!MANY && a.n_keep && (int64_t)(a.first ? load_scalar(a.first + blockIdx.y) : 0) + (int)blockIdx.x * (UNITS * AT_ONCE) >= load_scalar(a.n_keep + blockIdx.y)) return;
+  RowsOf<UNITS, MANY> rows(a, unit);
   int valid[AT_ONCE];
-#pragma unroll
-  for (int u = 0; u < AT_ONCE; ++u) valid[u] = a.n_keep ? a.n_keep[rows.bh[u]] : a.capacity;
+  rows.of(a.n_keep, a.capacity, valid);
   uint32_t x[AT_ONCE][WORDS], byte[AT_ONCE];
   char *to[AT_ONCE];
 #pragma unroll
   for (int u = 0; u < AT_ONCE; ++u) {
-    if (rows.place[u] >= valid[u]) rows.place[u] = -1;
+    rows.there[u] = rows.there[u] && rows.place[u] < valid[u];
     const int b = divide((uint32_t)rows.bh[u], a.kv_magic), h = rows.bh[u] - b * a.Hkv;
     const char *in = codes + (b * a.c_sb + h * a.c_sh + rows.place[u] * a.c_st) + lane * (WORDS * 4);
-    if (rows.place[u] >= 0) {
-      if constexpr (WORDS == 2) { const u32x2 w = *(const u32x2 *)in; x[u][0] = w[0]; x[u][1] = w[1]; }
-      else x[u][0] = *(const uint32_t *)in;
-      byte[u] = scales[((int64_t)rows.bh[u] * a.capacity + rows.place[u]) * SB + lane / 4];
-    }
-    to[u] = rows.place[u] < 0 ? nullptr : plain + (b * a.r_sb + h * a.r_sh + rows.r[u] * a.r_st) + lane * (DT == DT_F32 ? 32 : 16);
+    if constexpr (WORDS == 2) { const u32x2 w = *(const u32x2 *)in; x[u][0] = w[0]; x[u][1] = w[1]; }
+    else x[u][0] = *(const uint32_t *)in;
+    byte[u] = scales[((int64_t)rows.bh[u] * a.capacity + rows.place[u]) * SB + lane / 4];
+    to[u] = plain + (b * a.r_sb + h * a.r_sh + rows.r[u] * a.r_st) + lane * (DT == DT_F32 ? 32 : 16);
   }
 #pragma unroll
   for (int u = 0; u < AT_ONCE; ++u) {
-    if (!to[u]) continue;
+    if (!rows.there[u]) continue;
     const float scale = scale_of(byte[u]);
     if constexpr (DT == DT_BF16) {
       u32x4 y;
@@ -164,12 +194,16 @@ __global__ __launch_bounds__(QZ_THREADS) void dequantize_kernel(QuantizedArgs a,
 }
 
 template <int DT, int D, int FORMAT>
-hipError_t launch_as(bool back, const QuantizedArgs &a, const QuantizedLayers &layers, int32_t n_layers, hipStream_t stream) {
+hipError_t launch_as(bool back, QuantizedArgs a, const QuantizedLayers &layers, int32_t n_layers, hipStream_t stream) {
   constexpr int ROWS = QZ_THREADS / (D / 8) * AT_ONCE;
-  const int64_t total = (int64_t)a.heads * a.n_rows;
-  const dim3 grid((uint32_t)((total + ROWS - 1) / ROWS), 1, (uint32_t)n_layers * 2);
-  if (back) hipLaunchKernelGGL((dequantize_kernel<DT, D, FORMAT>), grid, dim3(QZ_THREADS), 0, stream, a, layers);
-  else hipLaunchKernelGGL((quantize_kernel<DT, D, FORMAT>), grid, dim3(QZ_THREADS), 0, stream, a, layers);
+  const bool many = a.n_rows <= ROWS / 2;
+  a.group = many ? ROWS / a.n_rows : 1;
+  a.rows_magic = division_magic(a.n_rows);          // (of numbers below ROWS)
+  const dim3 grid((uint32_t)(many ? 1 : (a.n_rows + ROWS - 1) / ROWS), (uint32_t)((a.heads + a.group - 1) / a.group), (uint32_t)n_layers * 2);
+#define WKV_QZ(KERNEL, MANY) hipLaunchKernelGGL((KERNEL<DT, D, FORMAT, MANY>), grid, dim3(QZ_THREADS), 0, stream, a, layers)
+  if (back) { if (many) WKV_QZ(dequantize_kernel, true); else WKV_QZ(dequantize_kernel, false); }
+  else { if (many) WKV_QZ(quantize_kernel, true); else WKV_QZ(quantize_kernel, false); }
+#undef WKV_QZ
   return hipGetLastError();
 }
 template <int DT>
