@@ -4,17 +4,18 @@
 // together, so that they leave in one store.  A workgroup takes rows of one (sequence, KV head), whose counts are scalars then, or, where there are
 // few rows to each, all rows of several: a token a sequence fills workgroups as well as a long prompt does.
 //
-// The 4128 kept rows a KV head of the 32K benchmark's prompt, four layers (102 MB), picked one by one from eight times as many: into 8 bits 37 us row by row with a lookup each, 29.5
-// with everything looked up at once, 22.3 = 4.6 TB/s with the plain rows read by nontemporal loads (a plain load leaves them in the memory-side cache, where nobody looks for them); the stores
-// are 8 of it.  Back 17.3 us = 5.9 TB/s.
+// The 4128 kept rows a KV head of the 32K benchmark's prompt, four layers (102 MB), picked one by one from eight times as many, into 8 bits: 37 us with each row's lookups
+// before its loads, 31 with all of a lane's lookups at once, 29.5 with the lookups as scalars and no load under a condition, 22.3 = 4.6 TB/s with the plain rows, which are read
+// once, by nontemporal loads (a ragged batch into 4 bits 27.4 and 21.5, a token for each of 64 sequences 3.5 both).  Back 16.7 us = 6.1 TB/s.
 #include "wkv_few_bits.h"
 
 namespace wkv {
 
 namespace {
 
-// Rows of a lane at once.  Two / four / eight, us: a token for each of 64 sequences, four layers, 3.4 / 4.4 / 5.9 into 8 bits, 3.2 / 3.8 / 4.7 back; the long calls above
-// 29.4 / 30.6 / 32.3 and 17.6 / 17.2 / 17.4 (workgroups of 64 to 256 threads the same).
+// Rows of a lane at once.  Two / four / eight, us, by workgroups of 128 before the nontemporal loads: a token for each of 64 sequences, four layers, 3.4 / 4.4 / 5.9 into 8 bits and
+// 3.2 / 3.8 / 4.7 back; the long call above 29.4 / 31.2 / 32.3 and 17.8 / 17.2 / 17.4; a ragged batch in 4 bits 27.4 / 27.8 / 29.2 and 21.3 / 19.2 / 20.2.  Two at once by workgroups
+// of 64 / 128 / 256: within 0.3 us of each other, but for the ragged batch: 26.7 / 27.4 / 27.4 and 25.9 / 21.3 / 21.1 back.
 constexpr int QZ_THREADS = 256, AT_ONCE = 2;
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
