@@ -693,7 +693,7 @@ wkv_status wkv_decode_tree(const wkv_tree_shape *shape, const void *q_new, const
  *   shape                the tree's (q, new and out strides and scale are not used, but must be valid)
  *   n_layers             1 .. WKV_MAX_LAYERS
  *   k_caches, v_caches   host arrays [n_layers] of device pointers; in place
- *   path                 device int32 [batch, n_nodes]: node numbers, strictly ascending as a path from the top is; entries past n_accept[b] are not read
+ *   path                 device int32 [batch, n_nodes]: node numbers, strictly ascending as a path from the top is; entries past n_accept[b] are not used
  *   n_accept             device int32 [batch], 0 .. n_nodes
  *   n_valid              device int32 [batch, n_kv_heads]
  * A path is taken as far as it ascends within 0 .. n_nodes - 1.  A (b, h) that could not take the tree is left as it is.  The rows behind the new count hold what they held.

@@ -120,7 +120,8 @@ wkv_status plan_rows(const wkv_quantized_shape *p, int32_t n_layers, const void 
 //   blocks   of 64 rows (two pairs of waves, the waves of a pair share a tile's keys) where there are no more; of 128; of 256 where these fill the compute units
 //            without ranges (64 sequences of 2000 rows and 64 nodes, 32q/8kv heads 180 us, by blocks of 128 215).  Of 32 rows, shared by two waves: never better than 64 (4 nodes over
 //            4128 rows 13.2 and 11.9 us, 64 sequences with 8 nodes 167.5 and 166.5).
-//   ranges   one / two / four / eight / 16 / 35: 16 nodes over 4128 rows, one sequence 120 / 66 / 38 / 23 / 15.5 / 17.8, eight - / 48 / 38 / 40 / 48 / -, 64 sequences 169 / 211 / ..
+//   ranges   one / two / four / eight / 16 / 32, us: 16 nodes over 4128 rows, one sequence 69 / 42 / 26 / 19 / 15.3 / 15.4, eight 70 / 48 / 38 / 40 / 47 / 53, 64 sequences
+//            170 / 210 / 234 / ..
 struct TreeCut {
   int32_t row_waves, key_waves, blocks, chunk, splits;
 };

@@ -5,6 +5,8 @@
 // Bound by memory, which every element crosses once each way.  The LPH = d / 16 lanes that hold a head's row add up its squares by DPP
 // steps; a lane keeps the weights of its 16 channels, of queries and of keys, in registers.  Everything else (whole lines in every load and store, five heads
 // of a token at once, fixed-point angles) is as for the rotation alone, wkv_rope.hip.
+// bf16, 32q/8kv heads of 128 channels: 64 tokens 4.5 us, a launch; 32768 tokens 115 us = 5.8 TB/s.  f16, 28q/4kv, 17027 tokens of three axes, interleaved, 58 us = 4.8 TB/s.
+// Fewer instructions (the root by the hardware's estimate, sine and cosine by a series of their own, weights selected in pairs) left all three times as they are.
 #include "wkv_device.h"
 #include "wkv_generation.h"
 
@@ -33,11 +35,13 @@ __device__ __forceinline__ float lanes_sum(float x) {
 //   by halves     lane p takes slots p, p + LPH, ..: piece j and its partner rotary / 2 channels on, E pairs
 //   interleaved   lane p takes pieces p, p + LPH, ..: E / 2 pairs each
 // Pieces past the rotary channels are normalised alone.
-constexpr int HEADS = 8, AT_ONCE = 5;
+// At once, two heads / five: the interleaved call above 58 / 63 us (96 and 134 registers), the one by halves of 32768 tokens 120 / 115.
+constexpr int HEADS = 8;
 template <int DT, int D, bool INTERLEAVED, bool AXES, bool STREAM>
 __global__ __launch_bounds__(NR_THREADS) void norm_rope_kernel(NormRopeArgs a, int32_t groups) {
   typedef typename Element<DT>::type T;
   typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
+  constexpr int AT_ONCE = INTERLEAVED ? 2 : 5;
   constexpr int E = 16 / sizeof(T), P = D / E, LPH = D / 16, N = P / LPH, TOKENS = NR_THREADS / LPH / HEADS;
   const int p = threadIdx.x % LPH, unit = threadIdx.x / LPH;
   const int64_t token = (int64_t)blockIdx.x * TOKENS + unit / HEADS;
@@ -90,7 +94,7 @@ __global__ __launch_bounds__(NR_THREADS) void norm_rope_kernel(NormRopeArgs a, i
       const char *in = (const char *)x.in + b * x.in_b + h * x.in_h + t * x.in_t;
       to[u] = (char *)x.out + b * x.out_b + h * x.out_h + t * x.out_t;
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[u][i] = *(const vec *)(in + at[i]);
+      for (int i = 0; i < N; ++i) v[u][i] = STREAM ? __builtin_nontemporal_load((const vec *)(in + at[i])) : *(const vec *)(in + at[i]);
     }
   };
   load();
@@ -178,7 +182,7 @@ hipError_t launch_d(const NormRopeArgs &a, hipStream_t stream) {
   // With few tokens a thread takes a single head, and the heads spread over the device.
   const bool few = x * groups <= 4096;
   const dim3 grid((uint32_t)x, (uint32_t)(few ? groups : 1));
-  // What exceeds the memory-side cache is not found there by whoever reads it next.
+  // What exceeds the memory-side cache is not found there by whoever reads it next, and is read and written past it: the 32K prompt 115 us, by plain loads 121.
   const bool streams = tokens * (a.q_heads + a.kv_heads) * D * elem_bytes(a.dtype) > MEMORY_CACHE_BYTES;
 #define WKV_NR(INTERLEAVED, AXES, STREAM) \
   hipLaunchKernelGGL((norm_rope_kernel<DT, D, INTERLEAVED, AXES, STREAM>), grid, dim3(NR_THREADS), 0, stream, a, few ? 1 : groups)

@@ -7,6 +7,8 @@
 // Key and value tiles reach LDS by DMA, a tile ahead.  A cache is read once for up to 256 rows, so a few nodes are bound by the stream of the cache and many by
 // the matrix pipe.  Where a wave's 32 rows are all there are, or half of them, the waves of a workgroup share the keys of a tile instead and join their results in LDS.
 //
+// bf16, 32q/8kv heads of 128 channels, 16 nodes over caches of 4128 rows: 64 sequences 168 us = 6.6 TB/s.
+//
 // How many rows a cache has is on the device: the ranges divide its capacity, and those behind its rows return at once.  The nodes' own tile, read from
 // the new rows, is a range of its own where there are several.  They are put into the cache at the end or by the second launch: nobody reads its rows from n on.
 #include "wkv_attention_tile.h"
@@ -510,7 +512,8 @@ __device__ __forceinline__ int accepted(const TreeArgs &a, const int32_t *__rest
 
 constexpr int ACCEPT_THREADS = 256;
 // Rows n + path[i] of one tensor and (sequence, KV head) into rows n + i.  All nodes' rows are asked for before the path is known, and every thread finds out
-// where its own go: two trips to memory instead of three.
+// where its own go: two trips to memory instead of three.  64 sequences with 16 nodes, 8 KV heads of 128 channels, bf16: 4.9 us; with the rows in an array under
+// conditions, which the compiler keeps outside the registers, 16.5.
 template <int PPR>
 __global__ __launch_bounds__(ACCEPT_THREADS) void accept_kernel(TreeArgs a, EvictLayers layers, const int32_t *__restrict__ path,
                                                                 const int32_t *__restrict__ n_accept, const int32_t *__restrict__ n_valid) {
