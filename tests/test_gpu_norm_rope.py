@@ -174,3 +174,45 @@ def test_captured_and_replayed(device):
         torch.cuda.synchronize()
         check(qo, *expected(q, qw, pos, inv, [0] * 64, 1e-6, 1.0, False), W.WKV_BF16)
         check(ko, *expected(k, kw, pos, inv, [0] * 64, 1e-6, 1.0, False), W.WKV_BF16)
+
+
+@pytest.mark.parametrize("dtype,d,interleaved,axes", [(W.WKV_BF16, 128, False, 1), (W.WKV_F16, 64, True, 3), (W.WKV_F32, 128, True, 1), (W.WKV_F32, 64, False, 2)])
+def test_calls_past_the_memory_side_cache(device, dtype, d, interleaved, axes):
+    # 300 MB of rows and more, in place, with padding among the tokens: the first tokens, the last ones and some between
+    Hq, H = 7, 4
+    T = 300 * 2 ** 20 // ((Hq + H) * d * TYPES[dtype].itemsize) + 3
+    g = torch.Generator(device=device).manual_seed(20)
+    rows = torch.randn((1, T, Hq + H, d), dtype=torch.float32, device=device, generator=g).to(TYPES[dtype])
+    pos = torch.arange(T, dtype=torch.int32, device=device)[None, :, None] + torch.arange(axes, dtype=torch.int32, device=device)
+    pos[0, 5::101, -1] = -1
+    inv, _ = W.wkv_rope_frequencies(d, 10000.0)
+    axis = [i % axes for i in range(d // 2)]
+    qw, kw = weights(d, dtype, device, 21), weights(d, dtype, device, 22)
+    at = torch.cat([torch.arange(0, 300), torch.arange(T // 2, T // 2 + 300), torch.arange(T - 300, T)]).to(device)
+    before, where = rows[:, at].clone(), pos[:, at]
+    n = (Hq + H) * d
+    strides = (T * n, d, n)
+    W.wkv_norm_rope(W.NormRopeShape(batch=1, n_tokens=T, n_q_heads=Hq, n_kv_heads=H, head_dim=d, dtype=dtype, inv_freq=inv, n_axes=axes, axis_of_pair=axis,
+                                    interleaved=interleaved, q_strides=strides, q_out_strides=strides, k_strides=strides, k_out_strides=strides),
+                    pos, qw, kw, rows, rows, rows[:, :, Hq:], rows[:, :, Hq:])
+    padding = where[0, :, -1] < 0
+    assert padding.any()
+    assert torch.equal(rows[:, at][:, padding], before[:, padding])
+    for part, w in ((slice(0, Hq), qw), (slice(Hq, Hq + H), kw)):
+        want, size = expected(before[:, ~padding, part].transpose(1, 2), w, where[:, ~padding], inv, axis, 1e-6, 1.0, interleaved)
+        check(rows[:, at][:, ~padding, part].transpose(1, 2), want, size, dtype)
+
+
+def test_offsets_past_32_bits(device):
+    # the second sequence 4.5 GiB behind the first, a second head 2.25 GiB behind the first
+    d, T, half, far = 128, 3, 2 ** 30 + 2 ** 27, 2 ** 31 + 2 ** 28 + 1024
+    buffer = torch.zeros(far + half + T * d, dtype=torch.bfloat16, device=device)
+    x = buffer.as_strided((2, 2, T, d), (far, half, d, 1))
+    x.copy_(torch.randn((2, 2, T, d), device=device, generator=torch.Generator(device=device).manual_seed(23)))
+    before = x.clone()
+    inv, _ = W.wkv_rope_frequencies(d, 10000.0)
+    pos = torch.tensor([[[0], [7], [100]], [[3], [4], [5]]], dtype=torch.int32, device=device)
+    w = weights(d, W.WKV_BF16, device, 24)
+    W.wkv_norm_rope(W.NormRopeShape(batch=2, n_tokens=T, n_q_heads=0, n_kv_heads=2, head_dim=d, dtype=W.WKV_BF16, inv_freq=inv,
+                                    k_strides=(far, half, d), k_out_strides=(far, half, d)), pos, None, w, None, None, x, x)
+    check(x, *expected(before, w, pos, inv, [0] * 64, 1e-6, 1.0, False), W.WKV_BF16)
