@@ -9,11 +9,11 @@
 // eight bits each, in columns of their own, and nothing is rounded to 16 bits (a 32-bit result would show it).  Up to four heads the three parts fit the columns;
 // five heads and more take a second product for the third part.
 //
-// Caches of 4128 rows, 32q/8kv heads of 128 channels, 8 bits: one sequence 7.0 us, 64 of them 90 us = 6.2 TB/s (103 before the codes came by nontemporal loads and scalar
-// addresses).  44 of 96 to 4500 rows, 28q/4kv, 4 bits, 20 us = 2.7 TB/s.  Blocks fetched two or three ahead: nothing or worse (94 us for the 64, 20.8 and 24.3 for the
+// Caches of 4128 rows, 32q/8kv heads of 128 channels, 8 bits: one sequence 7.0 us, 64 of them 87 us = 6.4 TB/s (103 before the codes came by nontemporal loads and scalar
+// addresses, 90 with 1536 ranges).  44 of 96 to 4500 rows, 28q/4kv, 4 bits, 19.4 us = 2.8 TB/s (20.0).  Blocks fetched two or three ahead: nothing or worse (with 1536 ranges 94 us for the 64, 20.8 and 24.3 for the
 // 44).  The merge is 4 to 5 us more.
 //
-// Key ranges, partial results and their merge are those of the decode step over plain caches (wkv_decode.hip).
+// Partial results and their merge are those of the decode step over plain caches (wkv_decode.hip); the key ranges are fewer (plan_quantized).
 #include "wkv_decode_parts.h"
 #include "wkv_few_bits.h"
 
