@@ -680,7 +680,8 @@ typedef struct {
  *   out                    device; must not overlap the inputs, nor a row another row
  * A (b, h) whose n_valid is negative or leaves no room for n_nodes rows keeps its caches; out is NaN for the nodes that exist.  Where a node's new value row holds an
  * infinity or a NaN, the rows of out of the nodes that attend to it are NaN, and no others; what padding holds shows nowhere.
- * Logits, softmax and sums are fp32; probabilities are rounded as at wkv_prefill_attention.  Workspace as at wkv_decode_step_quantized.
+ * Logits, softmax and sums are fp32 and the output is rounded once; in 16-bit types a probability reaches the product with the values as two numbers of the type
+ * (within 2^-15 of it in bf16, 2^-20 in fp16).  Workspace as at wkv_decode_step_quantized.
  */
 size_t wkv_tree_workspace_bytes(const wkv_tree_shape *shape);
 wkv_status wkv_decode_tree(const wkv_tree_shape *shape, const void *q_new, const void *k_new, const void *v_new, const int32_t *parent,

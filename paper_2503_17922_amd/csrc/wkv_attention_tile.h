@@ -56,8 +56,8 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b) {
 }
 
 // A row's reference moves when a logit exceeds it by LIFT + GROW (base 2), to LIFT below that logit: the largest probability of a row is 2^LIFT to 2^(LIFT + GROW).
-// For the product with the values 16-bit types round a probability to their own type, by half a step: an fp32 product takes eight times as long.  (Their sum, which the
-// normaliser needs in fp32, is of the unrounded ones.)  fp16 has all its bits from 2^-14 to 2^16 alone and nothing below 2^-25, so its probabilities are held high: what
+// For the product with the values 16-bit types round a probability to their own type, by half a step (the prompt attention; trees hold what that leaves in a second number): an fp32
+// product takes eight times as long.  (Their sum, which the normaliser needs in fp32, is of the unrounded ones.)  fp16 has all its bits from 2^-14 to 2^16 alone and nothing below 2^-25, so its probabilities are held high: what
 // it loses of a key is at most 2^-38 of the row's sum, and of 8192 keys, with values up to 1, no more than the rounding of an output in fp16 does.  Unlifted, a key of value zero that
 // stands 17 (base e) above 4096 others left a third of the output wrong.  GROW of 0 / 1 / 2 / 4 / 8, the packed prompts of 17.4K tokens
 // in fp16: 940 / 924 / 914 / 905 / 905 us.

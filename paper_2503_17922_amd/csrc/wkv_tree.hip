@@ -4,10 +4,14 @@
 // on the way to the top, a 64-bit mask a node.  One pass over the keys with a running reference and sum, transposed as in wkv_attention.hip:
 //   S^T = K Q^T    keys the A operand, 32 rows the B operand: lane l holds row l % 32 and half of the tile's keys
 //   O^T = V^T P^T  the probabilities as they lie in the lanes are the B operand, the values are read transposed
+// 16-bit types take a probability as two numbers, its upper bits and what they leave (8 + 8 bits, 11 + 11), each a product of its own with the same values: nothing but the output
+// is rounded to the type, as at a decode step.  With the upper part alone, rounded, outputs were 0.0024 (bf16; 0.00026 in fp16) of their root mean square off, more than the rounding of
+// an output, 0.0017 (0.0002).  It costs, a call: one sequence of 4128 rows and 16 nodes 15.6 -> 16.0 us, 64 of them 170 -> 173, eleven of mixed lengths and 64 nodes, 28q/4kv heads in fp16, 66 -> 77,
+// 64 of 2000 rows and 64 nodes 180 -> 225.  The lower products behind all upper ones of 16 keys: the same.
 // Key and value tiles reach LDS by DMA, a tile ahead.  A cache is read once for up to 256 rows, so a few nodes are bound by the stream of the cache and many by
 // the matrix pipe.  Where a wave's 32 rows are all there are, or half of them, the waves of a workgroup share the keys of a tile instead and join their results in LDS.
 //
-// bf16, 32q/8kv heads of 128 channels, 16 nodes over caches of 4128 rows: 64 sequences 168 us = 6.6 TB/s.
+// bf16, 32q/8kv heads of 128 channels, 16 nodes over caches of 4128 rows: 64 sequences 172 us = 6.3 TB/s.
 //
 // How many rows a cache has is on the device: the ranges divide its capacity, and those behind its rows return at once.  The nodes' own tile, read from
 // the new rows, is a range of its own where there are several.  They are put into the cache at the end or by the second launch: nobody reads its rows from n on.
@@ -46,6 +50,19 @@ struct Nodes {
     return (uint64_t)(uint32_t)__shfl((int)(uint32_t)(family >> 32), t) << 32 | (uint32_t)__shfl((int)(uint32_t)family, t);
   }
 };
+
+// Two floats as pairs of 16-bit numbers whose sums they are, but for what the second pair cannot hold: the upper bits, cut off, and what is left over of them.
+struct Parts { uint32_t upper, lower; };
+template <int DT>
+__device__ __forceinline__ Parts split_pair(float a, float b) {
+  if constexpr (DT == DT_F16) {
+    const auto h = __builtin_amdgcn_cvt_pkrtz(a, b);
+    return {__builtin_bit_cast(uint32_t, h), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a - (float)h[0], b - (float)h[1]))};
+  } else {
+    const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+    return {__builtin_amdgcn_perm(y, x, 0x07060302u), pack_pair<DT>(a - __uint_as_float(x & 0xffff0000u), b - __uint_as_float(y & 0xffff0000u))};
+  }
+}
 
 // Whether 16 bytes of a tensor are finite numbers.
 template <int DT>
@@ -256,8 +273,10 @@ __global__ __launch_bounds__((ROW_WAVES * KEY_WAVES * 64), (Shares<D, DT, ROW_WA
       for (int x = 0; x < KT * 2; ++x) {
         const f32x16 &p = s[x / 2];
         const int e = x % 2 * 8;
-        const bf16x8 pf = __builtin_bit_cast(bf16x8, make_uint4(pack_pair<DT>(p[e], p[e + 1]), pack_pair<DT>(p[e + 2], p[e + 3]),
-                                                                pack_pair<DT>(p[e + 4], p[e + 5]), pack_pair<DT>(p[e + 6], p[e + 7])));
+        const Parts w0 = split_pair<DT>(p[e], p[e + 1]), w1 = split_pair<DT>(p[e + 2], p[e + 3]), w2 = split_pair<DT>(p[e + 4], p[e + 5]),
+                    w3 = split_pair<DT>(p[e + 6], p[e + 7]);
+        const bf16x8 upper = __builtin_bit_cast(bf16x8, make_uint4(w0.upper, w1.upper, w2.upper, w3.upper));
+        const bf16x8 lower = __builtin_bit_cast(bf16x8, make_uint4(w0.lower, w1.lower, w2.lower, w3.lower));
 #pragma unroll
         for (int i = 0; i < VT; ++i) {
           const char *vp = vs + (x * 16 + y) * C::ROWB + C::value_slot(y, i * 4 + at * 2 + tl % 4 / 2) * 16 + tl % 2 * 8;
@@ -265,7 +284,8 @@ __global__ __launch_bounds__((ROW_WAVES * KEY_WAVES * 64), (Shares<D, DT, ROW_WA
           const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(__attribute__((address_space(3))) char *)vp);
           const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(__attribute__((address_space(3))) char *)(vp + 8 * C::ROWB));
           const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-          o[i] = mfma_step<DT, 32>(vf, pf, o[i]);
+          o[i] = mfma_step<DT, 32>(vf, upper, o[i]);
+          o[i] = mfma_step<DT, 32>(vf, lower, o[i]);
         }
       }
     }

@@ -1,0 +1,52 @@
+"""wkv_decode_tree in 16 bits rounds nothing but its output: against 64 bits, with what the types' own rounding allows and no more."""
+import math
+
+import pytest
+import torch
+
+import paper_2503_17922_amd as W
+from tests.test_gpu_tree import TYPES, Tree, families, some_tree
+
+pytestmark = pytest.mark.gpu
+
+# (counts, query heads, KV heads, channels, nodes): blocks of 64, 128 and 256 rows; one range, a few, many
+SHAPES = [([300, 77], 8, 2, 128, 16), ([4128], 32, 8, 128, 16), ([333, 0], 28, 4, 64, 20), ([900, 2000], 28, 4, 128, 64), ([200] * 40, 32, 8, 128, 64),
+          ([150] * 70, 16, 8, 64, 1)]
+
+
+@pytest.mark.parametrize("dtype", [W.WKV_BF16, W.WKV_F16])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: f"{len(s[0])}x{s[0][0]}-{s[1]}-{s[2]}-{s[3]}-{s[4]}")
+def test_only_the_output_is_rounded(device, dtype, shape):
+    counts, Hq, H, d, T = shape
+    s = Tree(device, counts, [some_tree(T, b) for b in range(len(counts))], Hq, H, d, dtype, max(counts) + T, seed=31)
+    s.step()
+    torch.cuda.synchronize()
+    G, t = Hq // H, TYPES[dtype]
+    half = torch.finfo(t).eps / 2
+    # A probability reaches the product as two numbers of the type, what the first leaves over in the second: 8 + 8 bits (2^-15 of it are left when both are cut off),
+    # 11 + 11 (2^-20; in fp16 numbers below 2^-14 have fewer bits, 2^-24 of a reference that is 2^13 and more: 2^-37 of the row's sum).
+    parts = 2.0 ** -15 if dtype == W.WKV_BF16 else 2.0 ** -20
+    off = total = 0.0
+    for b, n in enumerate(counts):
+        fam = families(s.parents[b])
+        hidden = torch.ones((T, n + T), dtype=torch.bool, device=device)
+        hidden[:, :n] = False
+        for i, f in enumerate(fam):
+            hidden[i, [n + j for j in f]] = False
+        for h in range(H):
+            k, v = (torch.cat([c[b, h, :n], x[b, h]]).double() for c, x in ((s.kc[0], s.kn), (s.vc[0], s.vn)))
+            q = s.q[b, h * G:(h + 1) * G].double()
+            p = torch.softmax((q @ k.t() * d ** -0.5).masked_fill(hidden, -math.inf), -1)
+            want, size = p @ v, p @ v.abs()
+            # logits, sums and joins as in test_gpu_tree.py
+            delta = (d + 4) * 2.0 ** -24 * d ** -0.5 * q.norm(dim=-1) * k.norm(dim=-1).max()
+            loose = 2 * delta + (2 * (n + T) + 128) * 2.0 ** -24
+            exact = size * (parts + loose[..., None])
+            tol = want.abs() * half + exact * (1 + half) + (n + T) * 2.0 ** -37 * v.abs().amax() + (2.0 ** -25 if t == torch.float16 else 1e-38)
+            err = (s.out[b, h * G:(h + 1) * G].double() - want).abs()
+            assert (err <= tol).all(), f"({b}, {h}): worst {float((err / tol).max())} of the tolerance"
+            off += float((err ** 2).sum())
+            total += float(((want.to(t).double() - want) ** 2).sum())
+    # and the root of the mean square is that of numbers rounded to the type: an error of 2^-15 at random beside one of 2^-8 adds 2^-14 of its square, and an
+    # average over 10^4 numbers and more leaves 1 %
+    assert off <= total * 1.02, math.sqrt(off / total)
