@@ -679,7 +679,8 @@ typedef struct {
  *   n_valid                device int32 [batch, n_kv_heads]; read
  *   out                    device; must not overlap the inputs, nor a row another row
  * A (b, h) whose n_valid is negative or leaves no room for n_nodes rows keeps its caches; out is NaN for the nodes that exist.  Where a node's new value row holds an
- * infinity or a NaN, the rows of out of the nodes that attend to it are NaN, and no others; what padding holds shows nowhere.
+ * infinity or a NaN, the rows of out of the nodes that attend to it are NaN, and no others.  A row of out is the same bits
+ * whatever the other nodes' queries are; what padding holds shows nowhere.
  * Logits, softmax and sums are fp32 and the output is rounded once; in 16-bit types a probability reaches the product with the values as two numbers of the type
  * (within 2^-15 of it in bf16, 2^-20 in fp16).  Workspace as at wkv_decode_step_quantized.
  */

@@ -238,7 +238,8 @@ __global__ __launch_bounds__((ROW_WAVES * KEY_WAVES * 64), (Shares<D, DT, ROW_WA
       top = fmaf(fmaxf(p.a, p.b), a.c1, -Reference<DT>::LIFT);
     }
     if (__any(top > m + Reference<DT>::GROW)) {
-      const float to = fmaxf(m, top), corr = to == -INFINITY ? 1.0f : fast_exp2(m - to);
+      // (each row's moves by its own logits alone: what the rows beside it hold, padding among them, does not show in its roundings)
+      const float to = top > m + Reference<DT>::GROW ? top : m, corr = to == -INFINITY ? 1.0f : fast_exp2(m - to);
       m = to;
       l *= corr;
 #pragma unroll

@@ -50,3 +50,29 @@ def test_only_the_output_is_rounded(device, dtype, shape):
     # and the root of the mean square is that of numbers rounded to the type: an error of 2^-15 at random beside one of 2^-8 adds 2^-14 of its square, and an
     # average over 10^4 numbers and more leaves 1 %
     assert off <= total * 1.02, math.sqrt(off / total)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("Hq,H,d,T,counts", [(8, 2, 128, 16, [300, 77]), (28, 4, 128, 40, [1000, 400]), (8, 2, 64, 40, [1500]), (32, 8, 128, 64, [120] * 33)])
+def test_a_row_does_not_depend_on_the_rows_beside_it(device, dtype, Hq, H, d, T, counts):
+    """Queries of other nodes, and what padding holds, change no bit of a node's output."""
+    parents = [some_tree(T, b) for b in range(len(counts))]
+    for p in parents:
+        p[T - 1] = -2                                          # one that does not exist
+    s = Tree(device, counts, parents, Hq, H, d, dtype, max(counts) + T, seed=32)
+    kept = list(range(0, T - 1, 3))
+    others = [i for i in range(T) if i not in kept]
+    s.step()
+    torch.cuda.synchronize()
+    first = s.out[:, :, kept].clone()
+    cache = [s.kc[0].clone(), s.vc[0].clone()]
+    for factor in (0.0, 6.0, -6.0, math.nan):
+        s.kc[0].copy_(cache[0])
+        s.vc[0].copy_(cache[1])
+        changed = s.q[:, :, others] * factor if factor == factor else torch.full_like(s.q[:, :, others], math.nan)
+        was = s.q[:, :, others].clone()
+        s.q[:, :, others] = changed
+        s.step()
+        torch.cuda.synchronize()
+        s.q[:, :, others] = was
+        assert torch.equal(s.out[:, :, kept], first), factor
