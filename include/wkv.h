@@ -575,7 +575,7 @@ typedef struct {
  *   k_weight      device [head_dim], 16-byte aligned, or NULL
  *   q_in ...      as at wkv_rope: 16-byte aligned, strides multiples of 16 bytes, in place with the same strides or without overlap
  * Without weights and with one axis the results are those of wkv_rope up to the order of their roundings.  The squares of a normalised row must sum to less
- * than fp32's largest number.  A row of zeros with eps = 0 gives NaN.  No workspace; calls on
+ * than fp32's largest number; how small they are does not matter, but a row of zeros with eps = 0 gives NaN.  No workspace; calls on
  * different streams may overlap in time.
  */
 wkv_status wkv_norm_rope(const wkv_norm_rope_shape *shape, const int32_t *positions, const void *q_weight, const void *k_weight,

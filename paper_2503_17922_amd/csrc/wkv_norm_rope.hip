@@ -15,6 +15,7 @@ namespace wkv {
 namespace {
 
 constexpr int NR_THREADS = 256;
+constexpr float TINY = 0x1p-100f;          // below it an eps is next to none
 
 template <int DT> struct Element;
 template <> struct Element<DT_BF16> { typedef __bf16 type; };
@@ -37,7 +38,8 @@ __device__ __forceinline__ float lanes_sum(float x) {
 // Pieces past the rotary channels are normalised alone.
 // At once, two heads / five: the interleaved call above 58 / 63 us (96 and 134 registers), the one by halves of 32768 tokens 120 / 115.
 constexpr int HEADS = 8;
-template <int DT, int D, bool INTERLEAVED, bool AXES, bool STREAM>
+// SMALL: a call with an eps below TINY.
+template <int DT, int D, bool INTERLEAVED, bool AXES, bool STREAM, bool SMALL>
 __global__ __launch_bounds__(NR_THREADS) void norm_rope_kernel(NormRopeArgs a, int32_t groups) {
   typedef typename Element<DT>::type T;
   typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
@@ -141,7 +143,23 @@ __global__ __launch_bounds__(NR_THREADS) void norm_rope_kernel(NormRopeArgs a, i
         for (int i = 0; i < N; ++i)
 #pragma unroll
           for (int e = 0; e < E; ++e) sum = fmaf(x[i][e], x[i][e], sum);
-        const float by = 1.0f / sqrtf(fmaf(lanes_sum<LPH>(sum), 1.0f / D, a.eps));
+        sum = lanes_sum<LPH>(sum);
+        float eps = a.eps;
+        // With no eps, or next to none, a row counts whose squares leave fp32's normal numbers: again, of the row times 2^100 (all its numbers are below 2^-50).  In a kernel
+        // of its own: where interleaved it takes 105 registers instead of 96, and the call above 59 us instead of 57.
+        if (SMALL && sum < TINY) {
+          sum = 0.0f;
+#pragma unroll
+          for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+              x[i][e] *= 1.0f / TINY;
+              sum = fmaf(x[i][e], x[i][e], sum);
+            }
+          sum = lanes_sum<LPH>(sum);
+          eps = eps * (1.0f / TINY) * (1.0f / TINY);
+        }
+        const float by = 1.0f / sqrtf(fmaf(sum, 1.0f / D, eps));
 #pragma unroll
         for (int i = 0; i < N; ++i)
 #pragma unroll
@@ -184,15 +202,16 @@ hipError_t launch_d(const NormRopeArgs &a, hipStream_t stream) {
   const dim3 grid((uint32_t)x, (uint32_t)(few ? groups : 1));
   // What exceeds the memory-side cache is not found there by whoever reads it next, and is read and written past it: the 32K prompt 115 us, by plain loads 121.
   const bool streams = tokens * (a.q_heads + a.kv_heads) * D * elem_bytes(a.dtype) > MEMORY_CACHE_BYTES;
-#define WKV_NR(INTERLEAVED, AXES, STREAM) \
-  hipLaunchKernelGGL((norm_rope_kernel<DT, D, INTERLEAVED, AXES, STREAM>), grid, dim3(NR_THREADS), 0, stream, a, few ? 1 : groups)
-#define WKV_NR_AXES(INTERLEAVED, STREAM) \
-  if (a.n_axes > 1) WKV_NR(INTERLEAVED, true, STREAM); \
-  else WKV_NR(INTERLEAVED, false, STREAM)
+#define WKV_NR(INTERLEAVED, AXES, STREAM, SMALL) \
+  hipLaunchKernelGGL((norm_rope_kernel<DT, D, INTERLEAVED, AXES, STREAM, SMALL>), grid, dim3(NR_THREADS), 0, stream, a, few ? 1 : groups)
+#define WKV_NR_AXES(INTERLEAVED, STREAM, SMALL) \
+  if (a.n_axes > 1) WKV_NR(INTERLEAVED, true, STREAM, SMALL); \
+  else WKV_NR(INTERLEAVED, false, STREAM, SMALL)
+  const bool small = a.eps < TINY;          // (all of them by plain loads)
   if (a.interleaved) {
-    if (streams) { WKV_NR_AXES(true, true); } else { WKV_NR_AXES(true, false); }
+    if (small) { WKV_NR_AXES(true, false, true); } else if (streams) { WKV_NR_AXES(true, true, false); } else { WKV_NR_AXES(true, false, false); }
   } else {
-    if (streams) { WKV_NR_AXES(false, true); } else { WKV_NR_AXES(false, false); }
+    if (small) { WKV_NR_AXES(false, false, true); } else if (streams) { WKV_NR_AXES(false, true, false); } else { WKV_NR_AXES(false, false, false); }
   }
 #undef WKV_NR_AXES
 #undef WKV_NR
