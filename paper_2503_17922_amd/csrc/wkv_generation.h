@@ -32,7 +32,9 @@ struct QuantizedArgs {
   const int32_t *tok_idx, *n_keep, *first;     // wkv_cache_dequantize: n_keep is its n_valid
   int32_t group;                               // of the launch: (sequence, KV head) pairs to a workgroup; division_magic(n_rows)
   uint32_t rows_magic;
+  int32_t first_row;                           // of the launch, with rows of one pair to a workgroup
 };
+constexpr int32_t MOST_ROW_GROUPS = 1 << 22;   // workgroups of a launch along the rows: a grid holds fewer than 2^32 threads a dimension, so long calls are several launches
 hipError_t launch_quantize(const QuantizedArgs &a, const QuantizedLayers &layers, int32_t n_layers, hipStream_t stream);
 hipError_t launch_dequantize(const QuantizedArgs &a, const QuantizedLayers &layers, int32_t n_layers, hipStream_t stream);
 

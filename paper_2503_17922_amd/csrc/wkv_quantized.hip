@@ -43,7 +43,7 @@ struct RowsOf {
         r[u] = v - at * a.n_rows;
       } else {
         bh[u] = blockIdx.y;
-        r[u] = (int)blockIdx.x * (UNITS * AT_ONCE) + v;
+        r[u] = a.first_row + (int)blockIdx.x * (UNITS * AT_ONCE) + v;
         there[u] = r[u] < a.n_rows;
         r[u] = min(r[u], a.n_rows - 1);
       }
@@ -80,7 +80,7 @@ __global__ __launch_bounds__(QZ_THREADS) void quantize_kernel(QuantizedArgs a, Q
   char *codes = (char *)layers.codes[is_v][layer], *scales = (char *)layers.scales[is_v][layer];
   const int lane = threadIdx.x % LPR, unit = threadIdx.x / LPR;
 
-  if (!MANY && a.n_keep && (int)blockIdx.x * (UNITS * AT_ONCE) >= load_scalar(a.n_keep + blockIdx.y)) return;
+  if (!MANY && a.n_keep && a.first_row + (int)blockIdx.x * (UNITS * AT_ONCE) >= load_scalar(a.n_keep + blockIdx.y)) return;
   RowsOf<UNITS, MANY> rows(a, unit);
   int keep[AT_ONCE], from[AT_ONCE];
   rows.of(a.n_keep, a.n_rows, keep);
@@ -148,7 +148,7 @@ __global__ __launch_bounds__(QZ_THREADS) void dequantize_kernel(QuantizedArgs a,
   const uint8_t *scales = (const uint8_t *)layers.scales[is_v][layer];
   const int lane = threadIdx.x % LPR, unit = threadIdx.x / LPR;
 
-  if (!MANY && a.n_keep && (int64_t)(a.first ? load_scalar(a.first + blockIdx.y) : 0) + (int)blockIdx.x * (UNITS * AT_ONCE) >= load_scalar(a.n_keep + blockIdx.y)) return;
+  if (!MANY && a.n_keep && (int64_t)(a.first ? load_scalar(a.first + blockIdx.y) : 0) + a.first_row + (int)blockIdx.x * (UNITS * AT_ONCE) >= load_scalar(a.n_keep + blockIdx.y)) return;
   RowsOf<UNITS, MANY> rows(a, unit);
   int valid[AT_ONCE];
   rows.of(a.n_keep, a.capacity, valid);
@@ -200,12 +200,18 @@ hipError_t launch_as(bool back, QuantizedArgs a, const QuantizedLayers &layers, 
   const bool many = a.n_rows <= ROWS / 2;
   a.group = many ? ROWS / a.n_rows : 1;
   a.rows_magic = division_magic(a.n_rows);          // (of numbers below ROWS)
-  const dim3 grid((uint32_t)(many ? 1 : (a.n_rows + ROWS - 1) / ROWS), (uint32_t)((a.heads + a.group - 1) / a.group), (uint32_t)n_layers * 2);
+  const int64_t groups = many ? 1 : ((int64_t)a.n_rows + ROWS - 1) / ROWS;
+  for (int64_t at = 0; at < groups; at += MOST_ROW_GROUPS) {
+    a.first_row = (int32_t)(at * ROWS);
+    const dim3 grid((uint32_t)(groups - at < MOST_ROW_GROUPS ? groups - at : MOST_ROW_GROUPS), (uint32_t)((a.heads + a.group - 1) / a.group), (uint32_t)n_layers * 2);
 #define WKV_QZ(KERNEL, MANY) hipLaunchKernelGGL((KERNEL<DT, D, FORMAT, MANY>), grid, dim3(QZ_THREADS), 0, stream, a, layers)
-  if (back) { if (many) WKV_QZ(dequantize_kernel, true); else WKV_QZ(dequantize_kernel, false); }
-  else { if (many) WKV_QZ(quantize_kernel, true); else WKV_QZ(quantize_kernel, false); }
+    if (back) { if (many) WKV_QZ(dequantize_kernel, true); else WKV_QZ(dequantize_kernel, false); }
+    else { if (many) WKV_QZ(quantize_kernel, true); else WKV_QZ(quantize_kernel, false); }
 #undef WKV_QZ
-  return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 template <int DT>
 hipError_t launch_type(bool back, const QuantizedArgs &a, const QuantizedLayers &layers, int32_t n_layers, hipStream_t stream) {
