@@ -36,7 +36,8 @@ __device__ __forceinline__ float lanes_sum(float x) {
 //   by halves     lane p takes slots p, p + LPH, ..: piece j and its partner rotary / 2 channels on, E pairs
 //   interleaved   lane p takes pieces p, p + LPH, ..: E / 2 pairs each
 // Pieces past the rotary channels are normalised alone.
-// At once, two heads / five: the interleaved call above 58 / 63 us (96 and 134 registers), the one by halves of 32768 tokens 120 / 115.
+// At once, two heads / five: the interleaved call above 57 / 62 us (96 and 134 registers), the one by halves of 32768 tokens 119 / 115.  In fp32 the same: interleaved with three axes (the call
+// above) 100 / 104, by halves 32768 tokens 258 / 253 = 5.3 TB/s, 16000 tokens with three axes 121 / 117; but 6000 by halves 50 / 53.
 constexpr int HEADS = 8;
 // SMALL: a call with an eps below TINY.
 template <int DT, int D, bool INTERLEAVED, bool AXES, bool STREAM, bool SMALL>
@@ -197,8 +198,10 @@ hipError_t launch_d(const NormRopeArgs &a, hipStream_t stream) {
   constexpr int TOKENS = NR_THREADS / (D / 16) / HEADS;
   const int64_t x = (tokens + TOKENS - 1) / TOKENS;
   const int32_t groups = (a.q_heads + a.kv_heads + HEADS - 1) / HEADS;
-  // With few tokens a thread takes a single head, and the heads spread over the device.
-  const bool few = x * groups <= 4096;
+  // With few tokens a thread takes a single head, and the heads spread over the device.  A head / all heads to a thread, us, 32q/8kv heads of 128 channels in bf16: 16 tokens 4.6 / 6.1,
+  // 256 5.3 / 6.7, 700 6.8 / 7.0, 800 (1000 workgroups) 7.0 / 7.2, 900 8.5 / 7.4, 1024 8.8 / 7.8, 1200 9.3 / 9.8, 2048 13.3 / 11.4, 3276 18.3 / 15.3.  Of 64 channels 1600 tokens 6.9 / 7.2;
+  // 64q/8kv heads in fp32 400 tokens 9.6 / 11.1; interleaved, 28q/4kv, fp16 500 5.7 / 7.0, 800 7.6 / 7.3.
+  const bool few = x * groups <= 1024;
   const dim3 grid((uint32_t)x, (uint32_t)(few ? groups : 1));
   // What exceeds the memory-side cache is not found there by whoever reads it next, and is read and written past it: the 32K prompt 115 us, by plain loads 121.
   const bool streams = tokens * (a.q_heads + a.kv_heads) * D * elem_bytes(a.dtype) > MEMORY_CACHE_BYTES;
