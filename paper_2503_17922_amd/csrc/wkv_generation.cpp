@@ -124,13 +124,14 @@ wkv_status plan_rows(const wkv_quantized_shape *p, int32_t n_layers, const void 
 
 }  // namespace
 
-// How the work of a tree is cut: rows of a block and ranges of a cache, by an estimate of the time in us that takes every cache for nine tenths full.  Fitted to
-// 34 shapes, each timed with up to fifteen numbers of ranges and every kind of block: the cut that it takes is 3.5 % behind the best in the geometric mean, 14 % at worst.
+// How the work of a tree is cut: rows of a block and ranges of a cache, by an estimate of the time in us that takes every cache for nine tenths full.  Fitted to 34 shapes, each timed with up to
+// fifteen numbers of ranges and every kind of block, before 16-bit types took a probability in two parts.  On the present kernels the cut that it takes is 4.3 % behind the best in the geometric
+// mean, 15 % at worst and once 28 % (two sequences of 2000 and 1000 rows, 64 nodes, fp32: 12 ranges 68 us, 20 53); constants fitted anew 3.6 %.
 //   blocks   of 64 rows (two pairs of waves, the waves of a pair share a tile's keys) where there are no more; of 128; of 256 where these fill the compute units
-//            without ranges (64 sequences of 2000 rows and 64 nodes, 32q/8kv heads 180 us, by blocks of 128 215).  Of 32 rows, shared by two waves: never better than 64 (4 nodes over
-//            4128 rows 13.2 and 11.9 us, 64 sequences with 8 nodes 167.5 and 166.5).
-//   ranges   one / two / four / eight / 16 / 32, us: 16 nodes over 4128 rows, one sequence 69 / 42 / 26 / 19 / 15.3 / 15.4, eight 70 / 48 / 38 / 40 / 47 / 53, 64 sequences
-//            170 / 210 / 234 / ..
+//            without ranges (64 sequences of 2000 rows and 64 nodes, 32q/8kv heads 221 us, by blocks of 128 251).  For 64 rows by blocks of 128: 16 nodes over 4128 rows, 64 sequences 192 us for
+//            175, 32 of them 112 for 98, one the same.
+//   ranges   one / two / four / eight / 16 / 32, us: 16 nodes over 4128 rows, one sequence 79 / 47 / 29 / 20 / 16.2 / 16.3, eight 81 / 51 / 39 / 41 / 48 / 55, 64 sequences
+//            175 / 216 / 237 / ..
 struct TreeCut {
   int32_t row_waves, key_waves, blocks, chunk, splits;
 };
