@@ -592,7 +592,8 @@ wkv_status wkv_norm_rope(const wkv_norm_rope_shape *shape, const int32_t *positi
  * codes 0.  A group that holds an infinity, a NaN or a magnitude above 2^127 stands for NaN in all its channels (s = 255, codes 0).
  *
  * Tensors: codes uint8 [batch, n_kv_heads, capacity, bytes of a row] by the strides below; scales uint8
- * [batch, n_kv_heads, capacity, head_dim / 32], contiguous, 4-byte aligned; of keys and of values.
+ * [batch, n_kv_heads, capacity, head_dim / 32], contiguous, 4-byte aligned; of keys and of values.  Of the attention calls wkv_decode_step_quantized reads such caches; the
+ * weighted step, the eviction by its weights and trees of drafted tokens take plain caches (wkv_cache_dequantize goes back).
  */
 typedef enum { WKV_CACHE_E4M3 = 0, WKV_CACHE_E2M1 = 1 } wkv_cache_format;
 
@@ -638,7 +639,7 @@ wkv_status wkv_cache_dequantize(const wkv_quantized_shape *shape, int32_t n_laye
 
 /*
  * wkv_decode_step over caches in 8 or 4 bits: the new token's rows are appended as wkv_cache_quantize holds them, and attention runs over what the
- * caches then stand for.  q_new [batch, n_q_heads, head_dim] and k_new, v_new [batch, n_kv_heads, head_dim] contiguous, 16-byte
+ * caches then stand for.  Scaled logits must be below 10^7 in magnitude (fp32 holds none to within one from there on; a larger one may leave its row NaN).  q_new [batch, n_q_heads, head_dim] and k_new, v_new [batch, n_kv_heads, head_dim] contiguous, 16-byte
  * aligned; n_valid, out and a (b, h) that cannot take the new row as at wkv_decode_step.  Workspace: 256-byte aligned, contents on entry irrelevant; calls that
  * may overlap in time need workspaces of their own.
  */
@@ -682,7 +683,7 @@ typedef struct {
  * infinity or a NaN, the rows of out of the nodes that attend to it are NaN, and no others.  A row of out is the same bits
  * whatever the other nodes' queries are; what padding holds shows nowhere.
  * Logits, softmax and sums are fp32 and the output is rounded once; in 16-bit types a probability reaches the product with the values as two numbers of the type
- * (within 2^-15 of it in bf16, 2^-20 in fp16).  Workspace as at wkv_decode_step_quantized.
+ * (within 2^-15 of it in bf16, 2^-20 in fp16).  Scaled logits must be below 10^7 in magnitude, as at wkv_decode_step_quantized.  Workspace as at wkv_decode_step_quantized.
  */
 size_t wkv_tree_workspace_bytes(const wkv_tree_shape *shape);
 wkv_status wkv_decode_tree(const wkv_tree_shape *shape, const void *q_new, const void *k_new, const void *v_new, const int32_t *parent,

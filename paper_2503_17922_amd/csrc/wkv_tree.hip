@@ -11,7 +11,7 @@
 // Key and value tiles reach LDS by DMA, a tile ahead.  A cache is read once for up to 256 rows, so a few nodes are bound by the stream of the cache and many by
 // the matrix pipe.  Where a wave's 32 rows are all there are, or half of them, the waves of a workgroup share the keys of a tile instead and join their results in LDS.
 //
-// bf16, 32q/8kv heads of 128 channels, 16 nodes over caches of 4128 rows: 64 sequences 174 us = 6.2 TB/s.
+// bf16, 32q/8kv heads of 128 channels, 16 nodes over caches of 4128 rows: 64 sequences 175 us = 6.2 TB/s.
 //
 // How many rows a cache has is on the device: the ranges divide its capacity, and those behind its rows return at once.  The nodes' own tile, read from
 // the new rows, is a range of its own where there are several.  They are put into the cache at the end or by the second launch: nobody reads its rows from n on.

@@ -76,3 +76,32 @@ def test_a_row_does_not_depend_on_the_rows_beside_it(device, dtype, Hq, H, d, T,
         torch.cuda.synchronize()
         s.q[:, :, others] = was
         assert torch.equal(s.out[:, :, kept], first), factor
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("T,counts", [(16, [200, 3000]), (64, [700, 90])])
+def test_the_largest_logits(device, dtype, T, counts):
+    """Up to 10^7: a row is the value of its largest logit, where the others are a step of fp32's logits and more below."""
+    d = 128
+    s = Tree(device, counts, [some_tree(T, b) for b in range(2)], 8, 2, d, dtype, max(counts) + T, seed=33, spread=1.0, scale=1.0)
+    # queries of one channel, keys of -1 .. 1 in it: logits of 9.8e6 at most
+    big = 9.8e6 if dtype != W.WKV_F16 else 6.0e4
+    s.q.zero_()
+    s.q[..., 3] = big
+    for c in (s.kc[0], s.kn):
+        c[..., 3] = -c[..., 3].abs().clamp(0.25, 0.9)
+    scale = big / 9.8e6 if dtype != W.WKV_F16 else 9.8e6 / 6.0e4
+    top = [37, 60]                                             # a row of the cache
+    for b in range(2):
+        s.kc[0][b, :, top[b], 3] = 1.0
+    s.shape.c.scale = scale
+    s.step()
+    torch.cuda.synchronize()
+    for b in range(2):
+        want = s.vc[0][b, :, top[b]].repeat_interleave(4, 0)[:, None].expand(-1, T, -1)
+        # p v / p: the products with the value, the reciprocal and its product, and two rescalings of either side where ranges are joined: eight steps of 2^-24.  (A value of a 16-bit
+        # type is itself again when that is rounded to the type.)
+        if dtype == W.WKV_F32:
+            assert ((s.out[b].double() - want.double()).abs() <= want.double().abs() * 2.0 ** -21).all(), b
+        else:
+            assert torch.equal(s.out[b], want), b
